@@ -64,7 +64,7 @@ def _newest_dep(src):
     global _HEADERS
     if _HEADERS is None:
         hs = glob.glob(os.path.join(CSRC, "**", "*.h"), recursive=True)
-        hs.append(os.path.join(INCLUDE, "fluid.h"))
+        hs += glob.glob(os.path.join(INCLUDE, "*.h"))
         _HEADERS = max(os.path.getmtime(h) for h in hs)
     return max(os.path.getmtime(src), _HEADERS, os.path.getmtime(__file__))
 
@@ -74,9 +74,11 @@ def build(host_only=False, jobs=None, force=False):
         shutil.rmtree(BUILD)
     os.makedirs(LIBDIR, exist_ok=True)
     host_srcs = sorted(glob.glob(os.path.join(CSRC, "host", "*.cpp")))
-    core = [s for s in host_srcs if not s.endswith("host_stubs.cpp")]
-    stub = [s for s in host_srcs if s.endswith("host_stubs.cpp")]
-    hip_srcs = sorted(glob.glob(os.path.join(CSRC, "gpu", "*.hip")))
+    host_srcs += sorted(glob.glob(os.path.join(CSRC, "attn", "*.cpp")))
+    stubs = ("host_stubs.cpp", "backend_host.cpp")
+    core = [s for s in host_srcs if not s.endswith(stubs)]
+    stub = [s for s in host_srcs if s.endswith(stubs)]
+    hip_srcs = sorted(glob.glob(os.path.join(CSRC, "gpu", "*.hip")) + glob.glob(os.path.join(CSRC, "attn", "*.hip")))
     jobs_list = [(s, _obj(s, "host"), ["g++"] + CXXFLAGS) for s in core + stub]
     if not host_only:
         jobs_list += [(s, _obj(s, "gpu"), [HIPCC] + HIPFLAGS) for s in hip_srcs]

@@ -34,7 +34,7 @@ def runtime_library():
 
 def _compile(src):
     obj = os.path.join(BUILD, os.path.basename(src) + ".o")
-    deps = glob.glob(os.path.join(CSRC, "host", "*.h")) + [os.path.join(INCLUDE, "fluid.h"), src]
+    deps = glob.glob(os.path.join(CSRC, "*", "*.h")) + glob.glob(os.path.join(INCLUDE, "*.h")) + [src]
     if not (os.path.exists(obj) and os.path.getmtime(obj) >= max(os.path.getmtime(d) for d in deps)):
         subprocess.run(["g++"] + CXXFLAGS + ["-c", src, "-o", obj], check=True)
     return obj
@@ -43,7 +43,7 @@ def _compile(src):
 def build():
     os.makedirs(BUILD, exist_ok=True)
     os.makedirs(LIBDIR, exist_ok=True)
-    srcs = sorted(glob.glob(os.path.join(CSRC, "host", "*.cpp")))
+    srcs = sorted(glob.glob(os.path.join(CSRC, "host", "*.cpp")) + glob.glob(os.path.join(CSRC, "attn", "*.cpp")))
     with cf.ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 4)) as ex:
         objs = list(ex.map(_compile, srcs))
     lib = os.path.join(LIBDIR, "libfluid_host.so")

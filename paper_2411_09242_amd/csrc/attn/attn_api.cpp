@@ -1,0 +1,269 @@
+// Entry points of fluid_attention.h: argument checks and launch sizes.
+#include "fluid_attention.h"
+
+#include <cmath>
+#include <cstdint>
+
+#include "../host/handles.h"
+#include "backend.h"
+
+namespace fluid {
+
+namespace {
+
+constexpr int64_t kMostTokens = int64_t(1) << 30;  // positions and windows stay within int32 sums
+constexpr int64_t kMostGroups = (int64_t(1) << 31) - 1;
+
+void check_head_dim(int d) { require(d == 32 || d == 64 || d == 128, "head_dim must be 32, 64 or 128"); }
+
+TokensArg tokens_arg(const fluid_tokens* d, const void* p, const char* name) {
+  require(d != nullptr, std::string(name) + ": NULL description");
+  const std::string at = std::string(name) + ": ";
+  require(d->dtype == FLUID_F32 || d->dtype == FLUID_BF16, at + "dtype must be f32 or bf16");
+  require(d->batch >= 1 && d->tokens >= 1 && d->heads >= 1, at + "batch, tokens and heads must be at least 1");
+  require(d->tokens <= kMostTokens, at + "more than 2^30 tokens");
+  check_head_dim(d->head_dim);
+  const int32_t extent[3] = {d->batch, d->tokens, d->heads};
+  const int el = dtype_bytes(d->dtype);
+  TokensArg a{const_cast<void*>(p), 0, 0, 0, 1};
+  int64_t* const to[3] = {&a.sb, &a.st, &a.sh};
+  for (int i = 0; i < 3; ++i) {
+    if (extent[i] == 1) continue;  // its stride is never used
+    require(d->stride[i] >= 0 && d->stride[i] <= (int64_t(1) << 40), at + "strides must lie in 0 .. 2^40");
+    *to[i] = d->stride[i];
+    if (d->stride[i] * el % 16) a.vec = 0;
+  }
+  if ((uintptr_t)p % 16) a.vec = 0;
+  require((uintptr_t)p % el == 0, at + "misaligned for its type");
+  return a;
+}
+TokensArg tokens_data(const fluid_tokens* d, const void* p, const char* name) {
+  require(p != nullptr, std::string(name) + ": NULL data");
+  return tokens_arg(d, p, name);
+}
+
+int64_t block_bytes(const fluid_kv_cache* c) { return int64_t(5) * c->head_dim * c->page_tokens / 4; }
+
+KvArgs check_cache(const fluid_kv_cache* c) {
+  require(c != nullptr, "cache: NULL description");
+  require(c->n_pages >= 1 && c->kv_heads >= 1 && c->batch >= 1 && c->max_pages >= 1,
+          "cache: n_pages, kv_heads, batch and max_pages must be at least 1");
+  check_head_dim(c->head_dim);
+  int log = 5;
+  while (log < 10 && (1 << log) != c->page_tokens) ++log;
+  require((1 << log) == c->page_tokens, "cache: page_tokens must be a power of two, 32 .. 1024");
+  require(int64_t(c->max_pages) * c->page_tokens <= kMostTokens, "cache: a table row names more than 2^30 tokens");
+  require(c->table_stride >= c->max_pages && c->table_stride <= (int64_t(1) << 40), "cache: table_stride below max_pages");
+  KvArgs a{};
+  a.table_stride = c->table_stride;
+  a.block = block_bytes(c);
+  a.n_pages = c->n_pages;
+  a.log_page = log;
+  a.kv_heads = c->kv_heads;
+  a.capacity = c->max_pages * c->page_tokens;
+  return a;
+}
+KvArgs check_pool(const fluid_kv_cache* c, const void* pool, const int32_t* pages) {
+  KvArgs a = check_cache(c);
+  require(pool != nullptr && pages != nullptr, "cache: NULL pool or page table");
+  require((uintptr_t)pool % 16 == 0, "cache: the pool must be 16-byte aligned");
+  a.pool = (uint8_t*)const_cast<void*>(pool);
+  a.pages = pages;
+  return a;
+}
+
+void kv_io(const fluid_kv_cache* cache, const void* pool, const int32_t* pages, const fluid_tokens* kd, const void* k,
+           const fluid_tokens* vd, const void* v, const int32_t* start, const int32_t* count, void* stream, bool write) {
+  KvIoParams p{};
+  p.c = check_pool(cache, pool, pages);
+  p.k = tokens_data(kd, k, "k");
+  p.v = tokens_data(vd, v, "v");
+  require(start != nullptr, "start: NULL");
+  require(kd->dtype == vd->dtype && kd->tokens == vd->tokens, "k and v must have one dtype and as many tokens");
+  for (const fluid_tokens* d : {kd, vd})
+    require(d->batch == cache->batch && d->heads == cache->kv_heads && d->head_dim == cache->head_dim,
+            "k and v must have the cache's batch, kv_heads and head_dim");
+  p.start = start;
+  p.count = count;
+  p.tokens = kd->tokens;
+  p.octets = (kd->tokens + 6) / 8 + 1;
+  p.items = int64_t(cache->batch) * p.octets * cache->kv_heads;
+  require(p.items * (cache->head_dim / 16) / 8 < kMostGroups, "k, v: too large for one launch");
+  run_kv_io(p, kd->dtype, cache->head_dim, write, stream);
+}
+
+// How an attention is cut into workgroups: those that share a tile of rows
+// (its splits) take chunks of its token tiles.
+void plan_splits(AttnParams& p, int64_t visible, int64_t target, int64_t least) {
+  const int64_t items = int64_t(p.batch) * p.kv_heads * p.row_tiles;
+  const int64_t tiles = visible / p.token_tile + 2;
+  int64_t splits = (target + items - 1) / items;
+  splits = std::max<int64_t>(1, std::min(splits, tiles / least));
+  p.chunk = (int32_t)((tiles + splits - 1) / splits);
+  p.splits = (int32_t)((tiles + p.chunk - 1) / p.chunk);
+  require(items * p.splits < kMostGroups && items * p.row_tile < kMostGroups, "q: too large for one launch");
+}
+uint64_t workspace_of(const AttnParams& p, int head_dim) {
+  return p.splits == 1 ? 0
+                       : uint64_t(p.batch) * p.kv_heads * p.row_tiles * p.splits * p.row_tile * (head_dim + 2) * 4;
+}
+void set_workspace(AttnParams& p, int head_dim, void* ws, uint64_t bytes) {
+  const uint64_t need = workspace_of(p, head_dim);
+  if (need == 0) return;
+  if (ws == nullptr || bytes < need)
+    fail(FLUID_E_ARENA_TOO_SMALL, "workspace: " + std::to_string(need) + " bytes needed, " +
+                                      std::to_string(ws ? bytes : 0) + " given");
+  require((uintptr_t)ws % 256 == 0, "workspace: must be 256-byte aligned");
+  p.ws = (float*)ws;
+}
+
+AttnParams check_opts(const fluid_attention_opts* o, const fluid_tokens* qd, int kv_heads) {
+  require(o != nullptr, "opts: NULL");
+  require(std::isfinite(o->scale) && o->scale > 0.0f, "opts: scale must be positive and finite");
+  require(o->causal == 0 || o->causal == 1, "opts: causal must be 0 or 1");
+  require(o->window >= 0 && o->sinks >= 0, "opts: window and sinks must not be negative");
+  require(qd->heads % kv_heads == 0, "q: heads must be a multiple of kv_heads");
+  AttnParams p{};
+  p.batch = qd->batch;
+  p.q_tokens = qd->tokens;
+  p.kv_heads = kv_heads;
+  p.group = qd->heads / kv_heads;
+  require(int64_t(p.q_tokens) * p.group <= kMostTokens, "q: more than 2^30 rows to a kv head");
+  p.causal = o->causal;
+  p.window = (int32_t)std::min<int64_t>(o->window, kMostTokens);
+  p.sinks = o->sinks;
+  p.cs = o->scale * 1.4426950408889634f;
+  return p;
+}
+void check_out(const fluid_tokens* qd, const fluid_tokens* od) {
+  require(od->dtype == qd->dtype && od->batch == qd->batch && od->tokens == qd->tokens && od->heads == qd->heads &&
+              od->head_dim == qd->head_dim,
+          "out must have q's dtype and shape");
+}
+// Tokens that a tile of rows can see, of `most`.
+int64_t visible_of(const AttnParams& p, int64_t most, int64_t queries) {
+  if (p.window == 0) return most;
+  return std::min(most, int64_t(p.window) * (p.causal ? 1 : 2) + queries + p.sinks);
+}
+
+// kv_max bounds the split alone; a cache that proves longer is shared in
+// larger chunks.
+AttnParams plan_kv_attention(const fluid_kv_cache* cache, const fluid_attention_opts* opts, int32_t kv_max,
+                             const fluid_tokens* qd) {
+  AttnParams p = check_opts(opts, qd, cache->kv_heads);
+  require(opts->causal == 1, "opts: attention over the cache is causal");
+  require(kv_max >= 1, "kv_max must be at least 1");
+  require(qd->batch == cache->batch && qd->head_dim == cache->head_dim, "q must have the cache's batch and head_dim");
+  p.kv_tokens = cache->max_pages * cache->page_tokens;
+  const int64_t rows = int64_t(p.q_tokens) * p.group;
+  p.row_tile = rows <= 16 ? 16 : 32;
+  p.token_tile = kKvTile;
+  p.row_tiles = (int32_t)((rows + p.row_tile - 1) / p.row_tile);
+  plan_splits(p, visible_of(p, std::min(kv_max, p.kv_tokens), std::min(p.q_tokens, p.row_tile / p.group + 1)), 1024, 8);
+  return p;
+}
+AttnParams plan_attention(const fluid_attention_opts* opts, const fluid_tokens* qd, const fluid_tokens* kd) {
+  AttnParams p = check_opts(opts, qd, kd->heads);
+  require(qd->dtype == kd->dtype && qd->batch == kd->batch && qd->head_dim == kd->head_dim,
+          "q and k must have one dtype, batch and head_dim");
+  p.kv_tokens = kd->tokens;
+  const int64_t rows = int64_t(p.q_tokens) * p.group;
+  p.row_tile = 128;
+  p.token_tile = qd->dtype == FLUID_BF16 ? 64 : 32;
+  p.row_tiles = (int32_t)((rows + p.row_tile - 1) / p.row_tile);
+  plan_splits(p, visible_of(p, p.kv_tokens, std::min(p.q_tokens, p.row_tile / p.group + 1)), 256, 4);
+  return p;
+}
+
+}  // namespace
+
+}  // namespace fluid
+
+using namespace fluid;
+
+extern "C" {
+
+fluid_status fluid_kv_pool_bytes(const fluid_kv_cache* cache, uint64_t* bytes) {
+  return call_guarded([&] {
+    check_cache(cache);
+    require(bytes != nullptr, "bytes: NULL");
+    *bytes = uint64_t(cache->n_pages) * cache->kv_heads * block_bytes(cache);
+  });
+}
+
+fluid_status fluid_kv_write(const fluid_kv_cache* cache, void* pool, const int32_t* pages, const fluid_tokens* kd,
+                            const void* k, const fluid_tokens* vd, const void* v, const int32_t* start,
+                            const int32_t* count, void* hip_stream) {
+  return call_guarded([&] { kv_io(cache, pool, pages, kd, k, vd, v, start, count, hip_stream, true); });
+}
+
+fluid_status fluid_kv_read(const fluid_kv_cache* cache, const void* pool, const int32_t* pages, const fluid_tokens* kd,
+                           void* k, const fluid_tokens* vd, void* v, const int32_t* start, const int32_t* count,
+                           void* hip_stream) {
+  return call_guarded([&] { kv_io(cache, pool, pages, kd, k, vd, v, start, count, hip_stream, false); });
+}
+
+fluid_status fluid_kv_attention_workspace(const fluid_kv_cache* cache, const fluid_attention_opts* opts,
+                                          int32_t kv_max, const fluid_tokens* qd, uint64_t* bytes) {
+  return call_guarded([&] {
+    check_cache(cache);
+    tokens_arg(qd, nullptr, "q");
+    require(bytes != nullptr, "bytes: NULL");
+    *bytes = workspace_of(plan_kv_attention(cache, opts, kv_max, qd), cache->head_dim);
+  });
+}
+
+fluid_status fluid_kv_attention(const fluid_kv_cache* cache, const void* pool, const int32_t* pages,
+                                const fluid_attention_opts* opts, int32_t kv_max, const fluid_tokens* qd,
+                                const void* q, const int32_t* q_len, const int32_t* kv_len, const fluid_tokens* od,
+                                void* out, void* workspace, uint64_t workspace_bytes, void* hip_stream) {
+  return call_guarded([&] {
+    const KvArgs c = check_pool(cache, pool, pages);
+    const TokensArg qa = tokens_data(qd, q, "q"), oa = tokens_data(od, out, "out");
+    check_out(qd, od);
+    require(kv_len != nullptr, "kv_len: NULL");
+    AttnParams p = plan_kv_attention(cache, opts, kv_max, qd);
+    p.c = c;
+    p.q = qa;
+    p.o = oa;
+    p.q_len = q_len;
+    p.kv_len = kv_len;
+    set_workspace(p, cache->head_dim, workspace, workspace_bytes);
+    run_kv_attention(p, qd->dtype, cache->head_dim, hip_stream);
+  });
+}
+
+fluid_status fluid_attention_workspace(const fluid_attention_opts* opts, const fluid_tokens* qd,
+                                       const fluid_tokens* kd, uint64_t* bytes) {
+  return call_guarded([&] {
+    tokens_arg(qd, nullptr, "q");
+    tokens_arg(kd, nullptr, "k");
+    require(bytes != nullptr, "bytes: NULL");
+    *bytes = workspace_of(plan_attention(opts, qd, kd), qd->head_dim);
+  });
+}
+
+fluid_status fluid_attention(const fluid_attention_opts* opts, const fluid_tokens* qd, const void* q,
+                             const fluid_tokens* kd, const void* k, const fluid_tokens* vd, const void* v,
+                             const int32_t* q_len, const int32_t* kv_len, const fluid_tokens* od, void* out,
+                             void* workspace, uint64_t workspace_bytes, void* hip_stream) {
+  return call_guarded([&] {
+    const TokensArg qa = tokens_data(qd, q, "q"), ka = tokens_data(kd, k, "k"), va = tokens_data(vd, v, "v"),
+                    oa = tokens_data(od, out, "out");
+    check_out(qd, od);
+    require(kd->dtype == vd->dtype && kd->batch == vd->batch && kd->tokens == vd->tokens && kd->heads == vd->heads &&
+                kd->head_dim == vd->head_dim,
+            "k and v must have one dtype and shape");
+    AttnParams p = plan_attention(opts, qd, kd);
+    p.q = qa;
+    p.k = ka;
+    p.v = va;
+    p.o = oa;
+    p.q_len = q_len;
+    p.kv_len = kv_len;
+    set_workspace(p, qd->head_dim, workspace, workspace_bytes);
+    run_attention(p, qd->dtype, qd->head_dim, hip_stream);
+  });
+}
+
+}  // extern "C"

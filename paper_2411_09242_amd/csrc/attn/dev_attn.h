@@ -1,0 +1,166 @@
+// Device helpers of the cache and attention kernels.
+#pragma once
+
+#include "../gpu/dev.h"
+#include "params.h"
+
+namespace fluid {
+
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+constexpr float kLow = -3.0e38f;  // a running maximum before the first score
+
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) {
+  return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+// over the four lanes of a quad
+__device__ __forceinline__ float quad_min(float v) {
+  v = fminf(v, dpp<0xB1>(v));
+  return fminf(v, dpp<0x4E>(v));
+}
+__device__ __forceinline__ float quad_max(float v) {
+  v = fmaxf(v, dpp<0xB1>(v));
+  return fmaxf(v, dpp<0x4E>(v));
+}
+
+// Element of a word that its nibble i holds (the inverse of
+// e -> (e >> 1) + 4 (e & 1)): nibbles i and i + 4 are neighbours, so that an
+// AND-OR makes a pair of f16 of them.
+__device__ __forceinline__ int nibble_element(int i) { return ((i & 3) << 1) | (i >> 2); }
+
+// The values of a word's elements 2 i and 2 i + 1 as one f16 pair: the two
+// nibbles moved to bits 6..9 of their halves and given the exponent of 16
+// read as 16 + n, and one fused multiply-add finishes b + s (16 + n).
+template <int I>
+__device__ __forceinline__ f16x2 nibble_pair(uint32_t w, f16x2 s, f16x2 b) {
+  const uint32_t x = I == 0 ? w << 6 : I == 1 ? w << 2 : I == 2 ? w >> 2 : w >> 6;
+  const f16x2 n = __builtin_bit_cast(f16x2, (x & 0x03C003C0u) | 0x4C004C00u);
+  return __builtin_elementwise_fma(n, s, b);
+}
+// A word's eight values, one (s, b) for all (K) or a pair per two (V).
+__device__ __forceinline__ f16x8 word_values(uint32_t w, const f16x2 s[4], const f16x2 b[4]) {
+  union { f16x2 h[4]; f16x8 v; } u;
+  u.h[0] = nibble_pair<0>(w, s[0], b[0]);
+  u.h[1] = nibble_pair<1>(w, s[1], b[1]);
+  u.h[2] = nibble_pair<2>(w, s[2], b[2]);
+  u.h[3] = nibble_pair<3>(w, s[3], b[3]);
+  return u.v;
+}
+__device__ __forceinline__ f16x8 word_values(uint32_t w, uint32_t pair) {
+  const f16x2 p = __builtin_bit_cast(f16x2, pair);
+  const f16x2 s = {p[0], p[0]}, b = {p[1], p[1]};
+  const f16x2 ss[4] = {s, s, s, s}, bb[4] = {b, b, b, b};
+  return word_values(w, ss, bb);
+}
+
+// Eight neighbouring elements as fp32; vec: the address is 16-byte aligned.
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, bool vec, float x[8]);
+template <>
+__device__ __forceinline__ void load8<float>(const float* p, bool vec, float x[8]) {
+  if (vec) {
+    const f32x4 a = ((const f32x4*)p)[0], b = ((const f32x4*)p)[1];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = a[i], x[4 + i] = b[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = p[i];
+  }
+}
+template <>
+__device__ __forceinline__ void load8<uint16_t>(const uint16_t* p, bool vec, float x[8]) {
+  if (vec) {
+    const uint4 a = *(const uint4*)p;
+    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(w[i] << 16), x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = bf16_to_f32(p[i]);
+  }
+}
+template <typename T>
+__device__ __forceinline__ void store8(T* p, bool vec, const float x[8]);
+template <>
+__device__ __forceinline__ void store8<float>(float* p, bool vec, const float x[8]) {
+  if (vec) {
+    ((f32x4*)p)[0] = f32x4{x[0], x[1], x[2], x[3]};
+    ((f32x4*)p)[1] = f32x4{x[4], x[5], x[6], x[7]};
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) p[i] = x[i];
+  }
+}
+template <>
+__device__ __forceinline__ void store8<uint16_t>(uint16_t* p, bool vec, const float x[8]) {
+  if (vec) {
+    *(uint4*)p = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) p[i] = f32_to_bf16(x[i]);
+  }
+}
+
+__device__ __forceinline__ int clamp_len(const int32_t* len, int b, int most) {
+  return len ? min(max(len[b], 0), most) : most;
+}
+
+// The tiles of `tile` tokens that rows at positions p_min .. p_max (of n
+// tokens) have to visit, numbered without gaps: first those of the sinks
+// before the window, then those from the window's start to the last token
+// seen.
+struct TileRange {
+  int sink_tiles, first, count;
+  __device__ __forceinline__ int tile(int u) const { return u < sink_tiles ? u : first + (u - sink_tiles); }
+};
+__device__ __forceinline__ TileRange tile_range(const AttnParams& p, int p_min, int p_max, int n, int tile) {
+  int hi = n, lo = 0, s = 0;
+  if (p.causal) hi = min(hi, p_max + 1);
+  else if (p.window > 0) hi = min(hi, p_max + p.window);
+  if (p.window > 0) {
+    lo = max(0, p_min - p.window + 1);
+    s = max(0, min(p.sinks, p.causal ? hi : n));
+  }
+  const int a = (s + tile - 1) / tile;
+  TileRange r;
+  if (hi <= lo) {
+    r.first = 0;
+    r.sink_tiles = r.count = a;
+  } else {
+    r.first = lo / tile;
+    r.sink_tiles = min(a, r.first);
+    r.count = r.sink_tiles + max((hi + tile - 1) / tile, a) - r.first;
+  }
+  return r;
+}
+
+// The tokens that the row at position `pos` sees: lo .. lo + span - 1 and those
+// below sinks.
+struct Sight {
+  int lo, span, sinks;
+  __device__ __forceinline__ bool sees(int t) const { return (uint32_t)(t - lo) < (uint32_t)span || t < sinks; }
+};
+__device__ __forceinline__ Sight sight(const AttnParams& p, int pos, int n) {
+  int hi = n;
+  Sight s = {0, 0, 0};
+  if (p.causal) hi = min(hi, pos + 1);
+  else if (p.window > 0) hi = min(hi, pos + p.window);
+  if (p.window > 0) {
+    s.lo = max(0, pos - p.window + 1);
+    s.sinks = min(p.sinks, p.causal ? hi : n);
+  }
+  s.span = max(0, hi - s.lo);
+  return s;
+}
+
+// Tiles of one share of a row tile's tokens.  The host's chunk fits the
+// longest cache it expects; a longer one makes larger shares.
+__device__ __forceinline__ int share_tiles(const AttnParams& p, const TileRange& r) {
+  return max(p.chunk, (r.count + p.splits - 1) / p.splits);
+}
+
+}  // namespace fluid

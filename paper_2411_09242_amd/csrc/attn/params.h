@@ -1,0 +1,53 @@
+// Launch parameters of the cache and attention kernels (host and device).
+#pragma once
+
+#include <stdint.h>
+
+namespace fluid {
+
+// A tensor of tokens: base and strides in elements; vec: every row starts on
+// a 16-byte address.
+struct TokensArg {
+  void* p;
+  int64_t sb, st, sh;
+  int32_t vec;
+};
+
+struct KvArgs {
+  uint8_t* pool;
+  const int32_t* pages;
+  int64_t table_stride;
+  int64_t block;  // bytes of one page of one kv head
+  int32_t n_pages, log_page, kv_heads;
+  int32_t capacity;  // tokens a row of the table can name
+};
+
+struct KvIoParams {
+  KvArgs c;
+  TokensArg k, v;
+  const int32_t* start;
+  const int32_t* count;
+  int32_t tokens;
+  int32_t octets;  // octets of tokens that T rows at any start can touch
+  int64_t items;   // batch * octets * kv_heads
+};
+
+// Rows are the (query, head of the group) pairs of one kv head, query slowest.
+struct AttnParams {
+  KvArgs c;        // kv_attention only
+  TokensArg q, k, v, o;
+  const int32_t* q_len;
+  const int32_t* kv_len;
+  int32_t batch, q_tokens, kv_tokens, kv_heads, group;
+  int32_t causal, window, sinks;
+  float cs;          // scale * log2(e)
+  int32_t row_tile, token_tile;  // rows and tokens of a workgroup's step
+  int32_t row_tiles; // tiles of rows of one kv head
+  int32_t splits;    // workgroups that share one tile of rows
+  int32_t chunk;     // least number of token tiles of such a share
+  float* ws;         // splits > 1: [item][split] of row_tile maxima, sums and rows of partial sums
+};
+
+constexpr int kKvTile = 32;  // tokens of a step over the 4-bit cache
+
+}  // namespace fluid
