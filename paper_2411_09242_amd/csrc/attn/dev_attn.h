@@ -32,57 +32,77 @@ __device__ __forceinline__ float quad_max(float v) {
 // AND-OR makes a pair of f16 of them.
 __device__ __forceinline__ int nibble_element(int i) { return ((i & 3) << 1) | (i >> 2); }
 
+// The two constants that make f16 of nibbles.  They are opaque to the compiler
+// so that each stays in a register: an AND-OR of literals is two instructions.
+struct Magic {
+  uint32_t mask, sixteen;
+  __device__ __forceinline__ Magic() {
+    asm("s_mov_b32 %0, 0x03c003c0" : "=s"(mask));
+    asm("v_mov_b32 %0, 0x4c004c00" : "=v"(sixteen));
+  }
+};
 // The values of a word's elements 2 i and 2 i + 1 as one f16 pair: the two
 // nibbles moved to bits 6..9 of their halves and given the exponent of 16
 // read as 16 + n, and one fused multiply-add finishes b + s (16 + n).
 template <int I>
-__device__ __forceinline__ f16x2 nibble_pair(uint32_t w, f16x2 s, f16x2 b) {
+__device__ __forceinline__ f16x2 nibble_pair(const Magic& mg, uint32_t w, f16x2 s, f16x2 b) {
   const uint32_t x = I == 0 ? w << 6 : I == 1 ? w << 2 : I == 2 ? w >> 2 : w >> 6;
-  const f16x2 n = __builtin_bit_cast(f16x2, (x & 0x03C003C0u) | 0x4C004C00u);
+  const f16x2 n = __builtin_bit_cast(f16x2, (x & mg.mask) | mg.sixteen);
   return __builtin_elementwise_fma(n, s, b);
 }
 // A word's eight values, one (s, b) for all (K) or a pair per two (V).
-__device__ __forceinline__ f16x8 word_values(uint32_t w, const f16x2 s[4], const f16x2 b[4]) {
+__device__ __forceinline__ f16x8 word_values(const Magic& mg, uint32_t w, const f16x2 s[4], const f16x2 b[4]) {
   union { f16x2 h[4]; f16x8 v; } u;
-  u.h[0] = nibble_pair<0>(w, s[0], b[0]);
-  u.h[1] = nibble_pair<1>(w, s[1], b[1]);
-  u.h[2] = nibble_pair<2>(w, s[2], b[2]);
-  u.h[3] = nibble_pair<3>(w, s[3], b[3]);
+  u.h[0] = nibble_pair<0>(mg, w, s[0], b[0]);
+  u.h[1] = nibble_pair<1>(mg, w, s[1], b[1]);
+  u.h[2] = nibble_pair<2>(mg, w, s[2], b[2]);
+  u.h[3] = nibble_pair<3>(mg, w, s[3], b[3]);
   return u.v;
 }
-__device__ __forceinline__ f16x8 word_values(uint32_t w, uint32_t pair) {
+__device__ __forceinline__ f16x8 word_values(const Magic& mg, uint32_t w, uint32_t pair) {
   const f16x2 p = __builtin_bit_cast(f16x2, pair);
   const f16x2 s = {p[0], p[0]}, b = {p[1], p[1]};
   const f16x2 ss[4] = {s, s, s, s}, bb[4] = {b, b, b, b};
-  return word_values(w, ss, bb);
+  return word_values(mg, w, ss, bb);
 }
 
-// Eight neighbouring elements as fp32; vec: the address is 16-byte aligned.
+// Eight neighbouring elements; vec: the address is 16-byte aligned.
 template <typename T>
-__device__ __forceinline__ void load8(const T* p, bool vec, float x[8]);
+struct Eight;
 template <>
-__device__ __forceinline__ void load8<float>(const float* p, bool vec, float x[8]) {
-  if (vec) {
-    const f32x4 a = ((const f32x4*)p)[0], b = ((const f32x4*)p)[1];
+struct Eight<float> {
+  f32x4 a, b;
+  __device__ __forceinline__ void load(const float* p, bool vec) {
+    if (vec) {
+      a = ((const f32x4*)p)[0];
+      b = ((const f32x4*)p)[1];
+    } else {
+      a = f32x4{p[0], p[1], p[2], p[3]};
+      b = f32x4{p[4], p[5], p[6], p[7]};
+    }
+  }
+  __device__ __forceinline__ void floats(float x[8]) const {
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[i] = a[i], x[4 + i] = b[i];
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = p[i];
   }
-}
+};
 template <>
-__device__ __forceinline__ void load8<uint16_t>(const uint16_t* p, bool vec, float x[8]) {
-  if (vec) {
-    const uint4 a = *(const uint4*)p;
-    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+struct Eight<uint16_t> {
+  uint32_t w[4];
+  __device__ __forceinline__ void load(const uint16_t* p, bool vec) {
+    if (vec) {
+      const uint4 a = *(const uint4*)p;
+      w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = p[2 * i] | ((uint32_t)p[2 * i + 1] << 16);
+    }
+  }
+  __device__ __forceinline__ void floats(float x[8]) const {
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(w[i] << 16), x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = bf16_to_f32(p[i]);
   }
-}
+};
 template <typename T>
 __device__ __forceinline__ void store8(T* p, bool vec, const float x[8]);
 template <>
@@ -105,8 +125,13 @@ __device__ __forceinline__ void store8<uint16_t>(uint16_t* p, bool vec, const fl
   }
 }
 
+// A value that all lanes read, by a scalar load: the lengths and page tables
+// are not written while a kernel runs.
+__device__ __forceinline__ int uniform_load(const int32_t* p, int64_t i) {
+  return ((const __attribute__((address_space(4))) int32_t*)p)[i];
+}
 __device__ __forceinline__ int clamp_len(const int32_t* len, int b, int most) {
-  return len ? min(max(len[b], 0), most) : most;
+  return len ? min(max(uniform_load(len, b), 0), most) : most;
 }
 
 // The tiles of `tile` tokens that rows at positions p_min .. p_max (of n
@@ -142,7 +167,7 @@ __device__ __forceinline__ TileRange tile_range(const AttnParams& p, int p_min, 
 // below sinks.
 struct Sight {
   int lo, span, sinks;
-  __device__ __forceinline__ bool sees(int t) const { return (uint32_t)(t - lo) < (uint32_t)span || t < sinks; }
+  __device__ __forceinline__ bool sees(int t) const { return (uint32_t)(t - lo) < (uint32_t)span | t < sinks; }
 };
 __device__ __forceinline__ Sight sight(const AttnParams& p, int pos, int n) {
   int hi = n;
@@ -157,10 +182,65 @@ __device__ __forceinline__ Sight sight(const AttnParams& p, int pos, int n) {
   return s;
 }
 
-// Tiles of one share of a row tile's tokens.  The host's chunk fits the
-// longest cache it expects; a longer one makes larger shares.
-__device__ __forceinline__ int share_tiles(const AttnParams& p, const TileRange& r) {
-  return max(p.chunk, (r.count + p.splits - 1) / p.splits);
-}
+// One tile of rows of one kv head, and the tiles of tokens it visits.
+struct Item {
+  int b, h, rt;
+  int n, rows, p0;  // tokens; rows of the kv head; position of row 0's query
+  int r0, r1;
+  TileRange range;
+  __device__ __forceinline__ void sequence(const AttnParams& p, int b_) {
+    b = b_;
+    n = clamp_len(p.kv_len, b, p.kv_tokens);
+    const int ql = clamp_len(p.q_len, b, p.q_tokens);
+    rows = ql * p.group;
+    p0 = n - ql;
+  }
+  __device__ __forceinline__ int p_min(const AttnParams& p) const { return p0 + (int)fdiv(r0, p.div_group); }
+  __device__ __forceinline__ int p_max(const AttnParams& p) const { return p0 + (int)fdiv(r1 - 1, p.div_group); }
+  // The row tile rt of the sequence; false if it has no rows.
+  __device__ __forceinline__ bool tile(const AttnParams& p, int rt_) {
+    rt = rt_;
+    r0 = rt * p.row_tile;
+    r1 = min(r0 + p.row_tile, rows);
+    if (r0 >= rows) return false;
+    range = tile_range(p, p_min(p), p_max(p), n, p.token_tile);
+    return true;
+  }
+};
+
+// What a workgroup works on: a run of an item's steps.  With p.splits shares
+// to an item each has p.chunk steps, or as many more as an item that proves
+// longer than the host expected needs; one that is shorter leaves the last
+// shares idle.  An item in one share is written by its workgroup, the others
+// are put together by the join.
+struct Share {
+  Item item;
+  int index, split;  // of the item and of its share
+  int shares;        // that the item has
+  int first, end;    // steps
+
+  __device__ __forceinline__ void steps(const AttnParams& p) {
+    const int per = max(p.chunk, (int)fdiv(item.range.count + p.splits - 1, p.div_splits));
+    shares = max(1, (item.range.count + per - 1) / per);
+    first = split * per;
+    end = min(first + per, item.range.count);
+  }
+  // false: nothing to do
+  __device__ __forceinline__ bool find(const AttnParams& p, int block) {
+    index = (int)fdiv(block, p.div_splits);
+    split = block - index * p.splits;
+    const int x = (int)fdiv(index, p.div_tiles), b = (int)fdiv(x, p.div_heads);
+    item.sequence(p, b);
+    item.h = x - b * p.kv_heads;
+    // row tiles from the last: with a causal mask the longest start first
+    if (!item.tile(p, p.row_tiles - 1 - (index - x * p.row_tiles))) return false;
+    steps(p);
+    return split < shares;
+  }
+  __device__ __forceinline__ bool whole() const { return shares == 1; }
+  __device__ __forceinline__ float* slot(const AttnParams& p, int head_dim) const {
+    return p.ws + ((int64_t)index * p.splits + split) * (p.row_tile * (head_dim + 2));
+  }
+};
 
 }  // namespace fluid

@@ -85,10 +85,10 @@ __global__ __launch_bounds__(256) void kv_write_kernel(KvIoParams p) {
   const Unit<D> u(p);
   if (!u.ok) return;  // whole half-wavefronts: the exchanges below stay within one
   const TokensArg& a = u.is_v ? p.v : p.k;
+  Eight<T> raw = {};
+  if (u.mine) raw.load((const T*)a.p + u.b * a.sb + u.row * a.st + u.h * a.sh + 32 * u.g + 8 * u.q, a.vec);
   float x[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = 0.0f;
-  if (u.mine) load8((const T*)a.p + u.b * a.sb + u.row * a.st + u.h * a.sh + 32 * u.g + 8 * u.q, a.vec, x);
+  raw.floats(x);
   float lo = 16384.0f, hi = -16384.0f, odd = 0.0f;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
@@ -151,7 +151,7 @@ __global__ __launch_bounds__(256) void kv_read_kernel(KvIoParams p) {
     pair = vp[0] | ((uint32_t)vp[8] << 16);
   }
   if (!u.mine) return;
-  const f16x8 v = word_values(w, pair);
+  const f16x8 v = word_values(Magic(), w, pair);
   float x[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) x[i] = (float)v[i];

@@ -14,7 +14,6 @@
 // Queries are scaled by a power of two per row before they become f16 (bf16
 // ones then are exact but for what lies 2^-14 below a row's largest); fp32
 // queries and probabilities are two f16 parts each and two products.
-// Probabilities are scaled by 2^15, where f16 has its whole range below them.
 //
 // The wavefronts of a workgroup take token tiles in turn and join their sums
 // in LDS; long caches are split over workgroups, joined by a second kernel.
@@ -25,8 +24,10 @@ namespace fluid {
 
 namespace {
 
-constexpr int kWaves = 4;
-constexpr float kPBits = 15.0f;
+// The running maximum may lag a row's largest score by kSlack powers of two, so
+// that the sums are hardly ever scaled; weights are scaled by 2^kPBits, at most
+// 2^15 then, where f16 has its whole range below them.
+constexpr float kSlack = 4.0f, kPBits = 15.0f - kSlack;
 
 __device__ __forceinline__ f32x4 mfma(f16x8 a, f16x8 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
@@ -45,9 +46,9 @@ template <int N>
 __device__ __forceinline__ void load_words(const uint8_t* p, uint32_t w[N]) {
   typedef uint32_t vec __attribute__((ext_vector_type(N)));
   if constexpr (N == 1) {
-    w[0] = *(const uint32_t*)p;
+    w[0] = __builtin_nontemporal_load((const uint32_t*)p);
   } else {
-    const vec v = *(const vec*)p;
+    const vec v = __builtin_nontemporal_load((const vec*)p);
 #pragma unroll
     for (int i = 0; i < N; ++i) w[i] = v[i];
   }
@@ -60,29 +61,43 @@ struct KvTile {
   uint32_t kw[2][G], kp[2][G];
   uint32_t vw[NC][WPL], vs[NC][4], vb[NC][4];
 
-  __device__ __forceinline__ void load(const uint8_t* blk, int P, int slot, int lane) {
-    const int m = lane & 15, g = lane >> 4;
-    const int t = slot + 8 * (m >> 2) + (m & 3);
-    const uint8_t* kpairs = blk + P * (D / 2);
-    const uint8_t* v = kpairs + P * (4 * G) + ((slot >> 3) + g) * (4 * D);
-    const uint8_t* vpairs = kpairs + P * (4 * G + D / 2) + ((slot >> 3) + g) * (32 * G);
+  // blk, P and slot are the same for all lanes; what a lane adds to the four
+  // parts' starts is not, but the same for every tile
+  struct Lane { uint32_t k, kp, v, vp; };
+  __device__ static __forceinline__ Lane lane_offsets(int lane) {
+    const int m = lane & 15, g = lane >> 4, t = 8 * (m >> 2) + (m & 3);
+    return {(uint32_t)(t * (D / 2) + g * (4 * G)), (uint32_t)(t * (4 * G)), (uint32_t)(g * (4 * D) + 4 * WPL * m),
+            (uint32_t)(g * (32 * G) + (D == 32 ? 0 : 32 * (m >> 3)))};
+  }
+  __device__ __forceinline__ void load_k(const uint8_t* blk, int P, int slot, const Lane& at) {
+    const uint8_t* const k = blk + slot * (D / 2);
+    const uint8_t* const kpairs = blk + P * (D / 2) + slot * (4 * G);
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      load_words<G>(blk + (t + 4 * i) * (D / 2) + g * (4 * G), kw[i]);
-      load_words<G>(kpairs + (t + 4 * i) * (4 * G), kp[i]);
+      load_words<G>(k + at.k + 4 * i * (D / 2), kw[i]);
+      load_words<G>(kpairs + at.kp + 4 * i * (4 * G), kp[i]);
     }
+  }
+  __device__ __forceinline__ void load_v(const uint8_t* blk, int P, int slot, const Lane& at) {
+    const uint8_t* const v = blk + P * (D / 2 + 4 * G) + slot * (D / 2);
+    const uint8_t* const vpairs = blk + P * (D + 4 * G) + slot * (4 * G);
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-      load_words<WPL>(v + 256 * c + 4 * WPL * m, vw[c]);
-      const uint8_t* sp = vpairs + 32 * (D == 32 ? 0 : 2 * c + (m >> 3));
-      load_words<4>(sp, vs[c]);
-      load_words<4>(sp + 16, vb[c]);
+      load_words<WPL>(v + at.v + 256 * c, vw[c]);
+      load_words<4>(vpairs + at.vp + 64 * c, vs[c]);
+      load_words<4>(vpairs + at.vp + 64 * c + 16, vb[c]);
     }
   }
 };
 
+// Whether the low f16 of w is an infinity or a NaN.
+__device__ __forceinline__ uint32_t odd_half(uint32_t w) { return (w & 0x7c00u) == 0x7c00u; }
+
+constexpr int kWaves = 4;
+
 template <typename T, int D, int MT>
-__global__ __launch_bounds__(64 * kWaves) void kv_attention_kernel(AttnParams p) {
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(MT == 1 ? 3 : 2)))
+void kv_attention_kernel(AttnParams p) {
   constexpr bool kTwo = sizeof(T) == 4;  // operands in two f16 parts
   constexpr int G = D / 32, R = 16 * MT;
   using Tile = KvTile<D>;
@@ -92,42 +107,57 @@ __global__ __launch_bounds__(64 * kWaves) void kv_attention_kernel(AttnParams p)
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, g4 = lane >> 4;
-  int x = blockIdx.x;
-  const int split = x % p.splits;
-  x /= p.splits;
-  const int item = x;
-  const int rt = x % p.row_tiles;
-  x /= p.row_tiles;
-  const int h = x % p.kv_heads, b = x / p.kv_heads;
+  const typename Tile::Lane at = Tile::lane_offsets(lane);
+  const int P = 1 << p.c.log_page;
+  const Magic mg;
 
-  const int n = clamp_len(p.kv_len, b, p.kv_tokens);
-  const int rows = clamp_len(p.q_len, b, p.q_tokens) * p.group;
-  const int r0 = rt * R, r1 = min(r0 + R, rows);
-  if (r0 >= rows) return;
-  const int p0 = n - rows / p.group;  // position of row 0's query
-  const int p_min = p0 + r0 / p.group, p_max = p0 + (r1 - 1) / p.group;
-  const TileRange range = tile_range(p, p_min, p_max, n, kKvTile);
-  const int per = share_tiles(p, range), shares = (range.count + per - 1) / per;
-  if (split >= max(shares, 1)) return;
-  const int u0 = split * per, u1 = min(u0 + per, range.count);
+  Share sh;
+  if (!sh.find(p, blockIdx.x)) return;
+  const Item& it = sh.item;
+  const int b = it.b, h = it.h, n = it.n, r0 = it.r0, r1 = it.r1, p0 = it.p0;
+  const int p_min = it.p_min(p), p_max = it.p_max(p);
+  const TileRange range = it.range;
+  const int u0 = sh.first, u1 = sh.end;
 
-  // queries, as the second operand: lane holds channels 32 j + 8 g4 .. +7 of
-  // its row
-  f16x8 qh[MT][G], ql[MT][kTwo ? G : 1];
-  float cs[MT];   // score to a power of two's exponent
+  // queries: a lane holds channels 32 j + 8 g4 .. +7 of its row
+  Eight<T> raw[MT][G];
   int pos[MT];
   Sight eye[MT];
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
     const int r = min(r0 + 16 * mt + col, r1 - 1);
-    const int i = r / p.group, hq = h * p.group + (r - i * p.group);
+    const int i = (int)fdiv(r, p.div_group), hq = h * p.group + (r - i * p.group);
     pos[mt] = p0 + i;
     eye[mt] = sight(p, pos[mt], n);
     const T* q = (const T*)p.q.p + b * p.q.sb + i * p.q.st + hq * p.q.sh + 8 * g4;
+#pragma unroll
+    for (int j = 0; j < G; ++j) raw[mt][j].load(q + 32 * j, p.q.vec);
+  }
+
+  const int32_t* const pages = p.c.pages + b * p.c.table_stride;
+  // A page outside the pool holds no tokens: its tiles are read from page 0 and
+  // none of their tokens is seen.
+  auto page_of = [&](int u) { return uniform_load(pages, (range.tile(u) * kKvTile) >> p.c.log_page); };
+  auto block = [&](int page) {
+    return p.c.pool + ((int64_t)((uint32_t)page < (uint32_t)p.c.n_pages ? page : 0) * p.c.kv_heads + h) * p.c.block;
+  };
+  auto slot = [&](int u) { return (range.tile(u) * kKvTile) & (P - 1); };
+  int u = u0 + wave, page = -1;
+  Tile tile;
+  if (u < u1) {
+    page = page_of(u);
+    tile.load_k(block(page), P, slot(u), at);
+    tile.load_v(block(page), P, slot(u), at);
+  }
+
+  f16x8 qh[MT][G], ql[MT][kTwo ? G : 1];
+  float cs[MT];  // the scale with the power of two taken out of the row
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
     float f[G][8], top = 0.0f;
 #pragma unroll
     for (int j = 0; j < G; ++j) {
-      load8(q + 32 * j, p.q.vec, f[j]);
+      raw[mt][j].floats(f[j]);
 #pragma unroll
       for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(f[j][e]));
     }
@@ -151,141 +181,134 @@ __global__ __launch_bounds__(64 * kWaves) void kv_attention_kernel(AttnParams p)
 
   float m[MT], l[MT];
   f32x4 acc[MT][NC][WPL];
-  const int P = 1 << p.c.log_page;
-  const int32_t* const pages = p.c.pages + b * p.c.table_stride;
-  auto page_of = [&](int u) -> int {
-    const int id = u < u1 ? pages[(range.tile(u) * kKvTile) >> p.c.log_page] : -1;
-    return id < p.c.n_pages ? id : -1;
-  };
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    m[mt] = kLow;
+    l[mt] = 0.0f;
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int j = 0; j < WPL; ++j) acc[mt][c][j] = f32x4{0, 0, 0, 0};
+  }
 
-  // A pass over the tokens; `safe` takes the rows of a tile with masked tokens
-  // one by one, which keeps what a masked token's value holds (0 times an
-  // infinity) out of the other rows.
-  auto pass = [&](bool safe) -> bool {
-    bool masked_any = false;
+  // A tile's keys are loaded once those of the tile before are used, its values
+  // likewise: about half a tile is always on its way, in the same registers.
+  while (u < u1) {
+    const int t0 = range.tile(u) * kKvTile;
+    const int after = min(u + kWaves, u1 - 1), next = page_of(after);
+    const bool dark = (uint32_t)page >= (uint32_t)p.c.n_pages;
+    // every row sees every token
+    const bool whole = !dark && t0 + kKvTile - 1 <= p_min &&
+                       (p.window <= 0 || t0 > p_max - p.window || t0 + kKvTile <= p.sinks);
+    f32x4 sc[MT][2];
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-      m[mt] = kLow;
-      l[mt] = 0.0f;
+    for (int i = 0; i < 2; ++i) {
 #pragma unroll
-      for (int c = 0; c < NC; ++c)
+      for (int mt = 0; mt < MT; ++mt) sc[mt][i] = f32x4{0, 0, 0, 0};
 #pragma unroll
-        for (int j = 0; j < WPL; ++j) acc[mt][c][j] = f32x4{0, 0, 0, 0};
+      for (int j = 0; j < G; ++j) {
+        const f16x8 k = word_values(mg, tile.kw[i][j], tile.kp[i][j]);
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+          if constexpr (kTwo) sc[mt][i] = mfma(k, ql[mt][j], sc[mt][i]);
+          sc[mt][i] = mfma(k, qh[mt][j], sc[mt][i]);
+        }
+      }
     }
-    for (int u = u0 + wave; u < u1; u += kWaves) {
-      const int t0 = range.tile(u) * kKvTile;
-      const int page = page_of(u);
-      if (page < 0) continue;
-      Tile tile;
-      tile.load(p.c.pool + ((int64_t)page * p.c.kv_heads + h) * p.c.block, P, t0 & (P - 1), lane);
-      // every row sees every token
-      const bool whole = t0 + kKvTile - 1 <= p_min &&
-                         (p.window <= 0 || t0 > p_max - p.window || t0 + kKvTile <= p.sinks);
-      masked_any |= !whole;
-      float s[MT][2][4];
+    tile.load_k(block(next), P, slot(after), at);
+    if (!whole) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        f32x4 sc[MT];
+      for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) sc[mt] = f32x4{0, 0, 0, 0};
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int j = 0; j < G; ++j) {
-          const f16x8 k = word_values(tile.kw[i][j], tile.kp[i][j]);
+          for (int r = 0; r < 4; ++r)
+            if (dark | !eye[mt].sees(t0 + 8 * g4 + 4 * i + r)) sc[mt][i][r] = -INFINITY;
+      // Weight 0 times a value that is no number would still be none.  So the
+      // groups that are none become zeros here, and NaN goes into the sums of
+      // the rows that do see them.
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        uint32_t odd = 0;  // of this lane's octet and group
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          odd |= (odd_half(tile.vs[c][i]) | odd_half(tile.vb[c][i])) << (2 * i);
+          odd |= (odd_half(tile.vs[c][i] >> 16) | odd_half(tile.vb[c][i] >> 16)) << (2 * i + 1);
+        }
+        if (__builtin_expect(__ballot(odd != 0) != 0, 0)) {
+          // a lane's sums belong to the channels 64 c + 16 g4 .. +15, of the
+          // group that the source lanes 8 (g4 / 2) of each sixteen hold
+          uint32_t of = 0;
+#pragma unroll
+          for (int o = 0; o < 4; ++o) of |= __shfl(odd, 16 * o + (D == 32 ? 0 : 8 * (g4 >> 1))) << (8 * o);
 #pragma unroll
           for (int mt = 0; mt < MT; ++mt) {
-            if constexpr (kTwo) sc[mt] = mfma(k, ql[mt][j], sc[mt]);
-            sc[mt] = mfma(k, qh[mt][j], sc[mt]);
+            bool hit = false;
+            for (int t = 0; t < kKvTile; ++t) hit |= !dark && (of >> t & 1) && eye[mt].sees(t0 + t);
+            if (hit) {
+#pragma unroll
+              for (int j = 0; j < WPL; ++j) acc[mt][c][j] = f32x4{NAN, NAN, NAN, NAN};
+            }
           }
-        }
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) s[mt][i][r] = sc[mt][r] * cs[mt];
-      }
-      if (!whole) {
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-          for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-              if (!eye[mt].sees(t0 + 8 * g4 + 4 * i + r)) s[mt][i][r] = -INFINITY;
-      }
-      f16x8 ph[MT], pl[kTwo ? MT : 1];
-#pragma unroll
-      for (int mt = 0; mt < MT; ++mt) {
-        float top = s[mt][0][0];
-#pragma unroll
-        for (int e = 1; e < 8; ++e) top = fmaxf(top, s[mt][e >> 2][e & 3]);
-        if (__ballot(top > m[mt])) {
-          const float m1 = fmaxf(m[mt], col_max(top));
-          const float a = __builtin_amdgcn_exp2f(m[mt] - m1);
-          m[mt] = m1;
-          l[mt] *= a;
-#pragma unroll
-          for (int c = 0; c < NC; ++c)
-#pragma unroll
-            for (int j = 0; j < WPL; ++j) acc[mt][c][j] *= a;
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float f = __builtin_amdgcn_exp2f(s[mt][e >> 2][e & 3] - m[mt] + kPBits);
-          l[mt] += f;
-          const _Float16 hi = (_Float16)f;
-          ph[mt][e] = hi;
-          if constexpr (kTwo) pl[mt][e] = (_Float16)(f - (float)hi);
-        }
-      }
-#pragma unroll
-      for (int c = 0; c < NC; ++c)
-#pragma unroll
-        for (int j = 0; j < WPL; ++j) {
-          f16x2 vs[4], vb[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            vs[i] = __builtin_bit_cast(f16x2, tile.vs[c][i]);
-            vb[i] = __builtin_bit_cast(f16x2, tile.vb[c][i]);
-          }
-          const f16x8 v = word_values(tile.vw[c][j], vs, vb);
-          if (!safe || whole) {
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-              if constexpr (kTwo) acc[mt][c][j] = mfma(v, pl[mt], acc[mt][c][j]);
-              acc[mt][c][j] = mfma(v, ph[mt], acc[mt][c][j]);
-            }
-          } else {
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-              f32x4 sum = acc[mt][c][j];
-              for (int row = 0; row < 16; ++row) {
-                const Sight other = sight(p, __shfl(pos[mt], row), n);
-                f16x8 w = v;
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                  if (!other.sees(t0 + 8 * g4 + e)) w[e] = (_Float16)0.0f;
-                f32x4 one = acc[mt][c][j];
-                if constexpr (kTwo) one = mfma(w, pl[mt], one);
-                one = mfma(w, ph[mt], one);
-                if (col == row) sum = one;
-              }
-              acc[mt][c][j] = sum;
-            }
+            const uint32_t keep = ((odd >> (2 * i)) & 1 ? 0u : 0xffffu) | ((odd >> (2 * i + 1)) & 1 ? 0u : 0xffff0000u);
+            tile.vs[c][i] &= keep;
+            tile.vb[c][i] &= keep;
           }
         }
+      }
     }
-    bool odd = false;
+    f16x8 ph[MT], pl[kTwo ? MT : 1];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
+      float top = sc[mt][0][0];
 #pragma unroll
-      for (int c = 0; c < NC; ++c)
+      for (int e = 1; e < 8; ++e) top = fmaxf(top, sc[mt][e >> 2][e & 3]);
+      top *= cs[mt];
+      if (__ballot(top > m[mt] + kSlack)) {
+        const float m1 = fmaxf(m[mt], col_max(top));
+        const float a = __builtin_amdgcn_exp2f(m[mt] - m1);
+        m[mt] = m1;
+        l[mt] *= a;
 #pragma unroll
-        for (int j = 0; j < WPL; ++j)
+        for (int c = 0; c < NC; ++c)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) odd |= !(fabsf(acc[mt][c][j][r]) <= 3.402823466e38f);
+          for (int j = 0; j < WPL; ++j) acc[mt][c][j] *= a;
+      }
+      const float shift = kPBits - m[mt];
+#pragma unroll
+      for (int e = 0; e < 8; e += 2) {
+        const f32x2 f = {__builtin_amdgcn_exp2f(__builtin_fmaf(sc[mt][e >> 2][e & 3], cs[mt], shift)),
+                         __builtin_amdgcn_exp2f(__builtin_fmaf(sc[mt][e >> 2][(e & 3) + 1], cs[mt], shift))};
+        l[mt] += f[0];
+        l[mt] += f[1];
+        const f16x2 hi = __builtin_convertvector(f, f16x2);
+        ph[mt][e] = hi[0], ph[mt][e + 1] = hi[1];
+        if constexpr (kTwo) pl[mt][e] = (_Float16)(f[0] - (float)hi[0]), pl[mt][e + 1] = (_Float16)(f[1] - (float)hi[1]);
+      }
     }
-    return masked_any && __ballot(odd) != 0;
-  };
-  if (pass(false)) pass(true);
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int j = 0; j < WPL; ++j) {
+        f16x2 vs[4], vb[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          vs[i] = __builtin_bit_cast(f16x2, tile.vs[c][i]);
+          vb[i] = __builtin_bit_cast(f16x2, tile.vb[c][i]);
+        }
+        const f16x8 v = word_values(mg, tile.vw[c][j], vs, vb);
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+          if constexpr (kTwo) acc[mt][c][j] = mfma(v, pl[mt], acc[mt][c][j]);
+          acc[mt][c][j] = mfma(v, ph[mt], acc[mt][c][j]);
+        }
+      }
+    tile.load_v(block(next), P, slot(after), at);
+    u += kWaves;
+    page = next;
+  }
 
   // join the wavefronts
 #pragma unroll
@@ -327,8 +350,8 @@ __global__ __launch_bounds__(64 * kWaves) void kv_attention_kernel(AttnParams p)
 #pragma unroll
       for (int e = 0; e < 8; ++e) o[e] += a * sh_o[w][r][c + e];
     }
-    if (shares > 1) {
-      float* to = p.ws + ((int64_t)item * p.splits + split) * (R * (D + 2));
+    if (!sh.whole()) {
+      float* to = sh.slot(p, D);
       if (c == 0) {
         to[r] = top;
         to[R + r] = sum;
@@ -339,26 +362,27 @@ __global__ __launch_bounds__(64 * kWaves) void kv_attention_kernel(AttnParams p)
       const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
 #pragma unroll
       for (int e = 0; e < 8; ++e) o[e] = sum == 0.0f ? 0.0f : o[e] * inv;
-      const int i = (r0 + r) / p.group, hq = h * p.group + (r0 + r - i * p.group);
+      const int i = (int)fdiv(r0 + r, p.div_group), hq = h * p.group + (r0 + r - i * p.group);
       store8((T*)p.o.p + b * p.o.sb + i * p.o.st + hq * p.o.sh + c, p.o.vec, o);
     }
   }
 }
 
-template <typename T, int D, int MT>
-hipError_t launch_rows(const AttnParams& p, hipStream_t s) {
-  const int64_t items = (int64_t)p.batch * p.kv_heads * p.row_tiles;
-  hipLaunchKernelGGL((kv_attention_kernel<T, D, MT>), dim3((uint32_t)(items * p.splits)), dim3(64 * kWaves), 0, s, p);
-  return hipGetLastError();
-}
 template <typename T>
 hipError_t launch(const AttnParams& p, int D, hipStream_t s) {
-  const bool two = p.row_tile == 32;
+  const dim3 grid((uint32_t)((int64_t)p.batch * p.kv_heads * p.row_tiles * p.splits)), block(64 * kWaves);
+#define FLUID_KV_D(N)                                                                                      \
+  case N:                                                                                                  \
+    if (p.row_tile == 16) hipLaunchKernelGGL((kv_attention_kernel<T, N, 1>), grid, block, 0, s, p);       \
+    else hipLaunchKernelGGL((kv_attention_kernel<T, N, 2>), grid, block, 0, s, p);                        \
+    break;
   switch (D) {
-    case 32: return two ? launch_rows<T, 32, 2>(p, s) : launch_rows<T, 32, 1>(p, s);
-    case 64: return two ? launch_rows<T, 64, 2>(p, s) : launch_rows<T, 64, 1>(p, s);
-    default: return two ? launch_rows<T, 128, 2>(p, s) : launch_rows<T, 128, 1>(p, s);
+    FLUID_KV_D(32)
+    FLUID_KV_D(64)
+    FLUID_KV_D(128)
   }
+#undef FLUID_KV_D
+  return hipGetLastError();
 }
 
 }  // namespace

@@ -3,6 +3,8 @@
 
 #include <stdint.h>
 
+#include "../host/kparams.h"
+
 namespace fluid {
 
 // A tensor of tokens: base and strides in elements; vec: every row starts on
@@ -42,10 +44,11 @@ struct AttnParams {
   int32_t causal, window, sinks;
   float cs;          // scale * log2(e)
   int32_t row_tile, token_tile;  // rows and tokens of a workgroup's step
-  int32_t row_tiles; // tiles of rows of one kv head
-  int32_t splits;    // workgroups that share one tile of rows
-  int32_t chunk;     // least number of token tiles of such a share
-  float* ws;         // splits > 1: [item][split] of row_tile maxima, sums and rows of partial sums
+  int32_t row_tiles;             // tiles of rows of one kv head
+  int32_t splits;  // most shares of an item, a workgroup each
+  int32_t chunk;   // steps of a share
+  FastDiv div_group, div_tiles, div_heads, div_splits;
+  float* ws;       // splits > 1: [item][split] of row_tile maxima, sums and rows of partial sums
 };
 
 constexpr int kKvTile = 32;  // tokens of a step over the 4-bit cache
