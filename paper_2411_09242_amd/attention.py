@@ -74,95 +74,99 @@ def _refuse(msg):
     raise fluid.FluidError(-1, msg)
 
 
-# Descriptions by what they describe (type, shape, strides): a decoding loop
-# makes the same few over and over, and filling a ctypes structure takes as
-# long as a small launch.
-_descs = {}
-
-
-def _tokens(t, name, device):
-    if t.dim() != 4:
-        _refuse(f"{name}: a tensor [batch, tokens, heads, head_dim] is needed, got {t.dim()} dimensions")
-    if t.device != device:
-        _refuse(f"{name}: on {t.device}, not on {device}")
-    shape, stride = t.shape, t.stride()
-    key = (t.dtype, shape, stride)
-    d = _descs.get(key)
-    if d is None:
-        torch = _torch()
-        if t.dtype not in (torch.float32, torch.bfloat16):
-            _refuse(f"{name}: dtype must be float32 or bfloat16, got {t.dtype}")
-        if stride[3] != 1 and shape[3] > 1:
-            _refuse(f"{name}: channels must be contiguous")
-        if max(shape) >= 1 << 31:
-            _refuse(f"{name}: too large")
-        if len(_descs) > 4096:
-            _descs.clear()
-        d = Tokens(fluid.F32 if t.dtype == torch.float32 else fluid.BF16, *shape, (C.c_int64 * 3)(*stride[:3]))
-        d = _descs[key] = (C.addressof(d), d)
-    return d[0]
-
-
 def _torch():
     import torch
     return torch
 
 
-def _ints(t, name, n, device):
-    """Address of an int32 tensor of n values; None stays None."""
+def _describe(t, name, device):
+    """fluid_tokens of a tensor, or a refusal."""
+    torch = _torch()
+    if t.dim() != 4:
+        _refuse(f"{name}: a tensor [batch, tokens, heads, head_dim] is needed, got {t.dim()} dimensions")
+    if t.get_device() != device:
+        _refuse(f"{name}: on {t.device}, not on GPU {device}")
+    if t.dtype not in (torch.float32, torch.bfloat16):
+        _refuse(f"{name}: dtype must be float32 or bfloat16, got {t.dtype}")
+    shape, stride = t.shape, t.stride()
+    if stride[3] != 1 and shape[3] > 1:
+        _refuse(f"{name}: channels must be contiguous")
+    if max(shape) >= 1 << 31:
+        _refuse(f"{name}: too large")
+    return Tokens(fluid.F32 if t.dtype == torch.float32 else fluid.BF16, *shape, (C.c_int64 * 3)(*stride[:3]))
+
+
+def _check_ints(t, name, n, device):
+    """Refuses what is no int32 tensor of n values; None is none."""
     if t is None:
-        return None
-    if t.dtype != _torch().int32 or t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1) or t.device != device:
-        _refuse(f"{name}: {n} contiguous int32 values on {device} are needed")
-    return t.data_ptr()
+        return
+    if (t.dtype != _torch().int32 or t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1)
+            or t.get_device() != device):
+        _refuse(f"{name}: {n} contiguous int32 values on GPU {device} are needed")
 
 
-def _cache(pool, pages, head_dim):
-    if pool.dim() != 3 or pool.element_size() != 1 or not pool.is_contiguous():
+def _describe_cache(pool, pages, head_dim, device):
+    torch = _torch()
+    if pool.dim() != 3 or pool.dtype != torch.uint8 or not pool.is_contiguous():
         _refuse("pool: a contiguous uint8 tensor [pages, kv_heads, block] is needed")
-    if pages.dim() != 2 or pages.dtype != _torch().int32 or (pages.shape[1] > 1 and pages.stride(1) != 1):
+    if pages.dim() != 2 or pages.dtype != torch.int32 or (pages.shape[1] > 1 and pages.stride(1) != 1):
         _refuse("pages: an int32 tensor [batch, max_pages] with contiguous rows is needed")
-    if pages.device != pool.device:
-        _refuse(f"pages: on {pages.device}, not on {pool.device}")
-    key = (pool.shape, pages.shape, pages.stride(), head_dim)
-    d = _descs.get(key)
-    if d is None:
-        n, heads, block = pool.shape
-        tokens = block * 4 // (5 * head_dim)
-        if block * 4 != 5 * head_dim * tokens or tokens not in PAGE_TOKENS:
-            _refuse(f"pool: a block of {block} bytes is no page of head_dim {head_dim}")
-        if len(_descs) > 4096:
-            _descs.clear()
-        stride = pages.stride(0) if pages.shape[0] > 1 else pages.shape[1]
-        d = CacheDesc(n, tokens, heads, head_dim, pages.shape[0], pages.shape[1], stride)
-        d = _descs[key] = (C.addressof(d), d)
-    return d[0]
+    if pool.get_device() != device or pages.get_device() != device:
+        _refuse(f"pool, pages: on {pool.device} and {pages.device}, not on GPU {device}")
+    n, heads, block = pool.shape
+    tokens = block * 4 // (5 * head_dim) if head_dim else 0
+    if block * 4 != 5 * head_dim * tokens or tokens not in PAGE_TOKENS:
+        _refuse(f"pool: a block of {block} bytes is no page of head_dim {head_dim}")
+    stride = pages.stride(0) if pages.shape[0] > 1 else pages.shape[1]
+    return CacheDesc(n, tokens, heads, head_dim, pages.shape[0], pages.shape[1], stride)
 
 
-def _opts(scale, causal, window, sinks, head_dim):
-    key = (scale, causal, window, sinks, head_dim)
-    d = _descs.get(key)
-    if d is None:
-        for name, v in (("window", window), ("sinks", sinks)):
-            if not 0 <= v < 1 << 31:
-                _refuse(f"{name}: {v} is out of range")
-        if len(_descs) > 4096:
-            _descs.clear()
-        d = Opts(1.0 / math.sqrt(head_dim) if scale is None else scale, 1 if causal else 0, window, sinks)
-        d = _descs[key] = (C.addressof(d), d)
-    return d[0]
+def _describe_opts(scale, causal, window, sinks, head_dim):
+    for name, v in (("window", window), ("sinks", sinks)):
+        if not 0 <= v < 1 << 31:
+            _refuse(f"{name}: {v} is out of range")
+    return Opts(1.0 / math.sqrt(head_dim) if scale is None else scale, 1 if causal else 0, window, sinks)
+
+
+# A call's checks and descriptions depend on its tensors' types, shapes,
+# strides and devices and on its numbers alone, and a decoding loop makes the
+# same few calls over and over: they are made once for each such set.  (Filling
+# and checking them takes 9 us, as long as a small kernel; finding them, 2.)
+_calls = {}
+
+
+def _form(t):
+    return None if t is None else (t.dtype, t.shape, t.stride(), t.get_device())
+
+
+def _keep(key, made):
+    if len(_calls) >= 4096:
+        _calls.clear()
+    _calls[key] = made
+    return made
+
+
+def _device_of(t, name):
+    if not t.is_cuda:
+        _refuse(f"{name}: a tensor on the GPU is needed, got {t.device}")
+    return t.get_device()
 
 
 def _stream(stream, device):
     if stream is None:
-        stream = _torch().cuda.current_stream(device)
+        return _torch().cuda.current_stream(device).cuda_stream
     return getattr(stream, "cuda_stream", stream)
 
 
-def _on_gpu(t, name):
-    if not t.is_cuda:
-        _refuse(f"{name}: a tensor on the GPU is needed, got {t.device}")
-    return t.device
+try:  # the same handle without a Stream object around it
+    from torch._C import _cuda_getCurrentRawStream as _raw_stream
+except ImportError:
+    def _raw_stream(device):
+        return _stream(None, device)
+
+
+def _addr(d):
+    return C.addressof(d)
 
 
 def pool_block(page_tokens, head_dim):
@@ -170,33 +174,46 @@ def pool_block(page_tokens, head_dim):
     return 5 * head_dim * page_tokens // 4
 
 
+def _io_call(pool, pages, k, v, start, count):
+    dev = _device_of(pool, "pool")
+    kd, vd = _describe(k, "k", dev), _describe(v, "v", dev)
+    c = _describe_cache(pool, pages, k.shape[3], dev)
+    _check_ints(start, "start", pages.shape[0], dev)
+    _check_ints(count, "count", pages.shape[0], dev)
+    if start is None:
+        _refuse("start: needed")
+    return (_lib(), dev, _addr(c), _addr(kd), _addr(vd), (c, kd, vd))
+
+
+def _io(write, pool, pages, k, v, start, count, stream):
+    key = (fluid._lib, pool.shape, pool.dtype, pool.get_device(), _form(pages), _form(k), _form(v), _form(start),
+           _form(count))
+    made = _calls.get(key)
+    if made is None:
+        made = _keep(key, _io_call(pool, pages, k, v, start, count))
+    lib, dev, c, kd, vd, _ = made
+    st = (lib.fluid_kv_write if write else lib.fluid_kv_read)(
+        c, pool.data_ptr(), pages.data_ptr(), kd, k.data_ptr(), vd, v.data_ptr(), start.data_ptr(),
+        None if count is None else count.data_ptr(), _raw_stream(dev) if stream is None else _stream(stream, dev))
+    if st:
+        fluid._check(st)
+
+
 def kv_write(pool, pages, k, v, start, count=None, stream=None):
     """Quantise tokens k, v [batch, T, kv_heads, head_dim] into the cache: row
     i of sequence b becomes token start[b] + i, for i < count[b] (None: all)."""
-    dev = _on_gpu(pool, "pool")
-    kd, vd = _tokens(k, "k", dev), _tokens(v, "v", dev)
-    n = pages.shape[0]
-    fluid._check(_lib().fluid_kv_write(
-        _cache(pool, pages, k.shape[3]), pool.data_ptr(), pages.data_ptr(), kd, k.data_ptr(), vd, v.data_ptr(),
-        _ints(start, "start", n, dev), _ints(count, "count", n, dev), _stream(stream, dev)))
+    _io(True, pool, pages, k, v, start, count, stream)
 
 
 def kv_read(pool, pages, start, k, v, count=None, stream=None):
     """The cache's values of tokens start[b] .. of every sequence into k, v
     [batch, T, kv_heads, head_dim], count[b] of them (None: T); rows past that
     are left as they are."""
-    dev = _on_gpu(pool, "pool")
-    kd, vd = _tokens(k, "k", dev), _tokens(v, "v", dev)
-    n = pages.shape[0]
-    fluid._check(_lib().fluid_kv_read(
-        _cache(pool, pages, k.shape[3]), pool.data_ptr(), pages.data_ptr(), kd, k.data_ptr(), vd, v.data_ptr(),
-        _ints(start, "start", n, dev), _ints(count, "count", n, dev), _stream(stream, dev)))
+    _io(False, pool, pages, k, v, start, count, stream)
 
 
 def _workspace(need, workspace, device, stream):
     """(tensor to keep for the call, address, bytes)."""
-    if need == 0:
-        return None, None, 0
     torch = _torch()
     if workspace is None:
         # torch hands a freed block out again only in the order of the stream
@@ -207,19 +224,29 @@ def _workspace(need, workspace, device, stream):
             s = stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(stream, device=device)
             with torch.cuda.stream(s):
                 workspace = torch.empty(need, dtype=torch.uint8, device=device)
+    elif workspace.get_device() != device or not workspace.is_contiguous():
+        _refuse(f"workspace: a contiguous tensor on GPU {device} is needed")
     return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def _kv_call(pool, pages, q, kv_len, q_len, kv_max, scale, window, sinks, out):
+    dev = _device_of(pool, "pool")
+    qd = _describe(q, "q", dev)
+    od = qd if out is None else _describe(out, "out", dev)
+    D, n = q.shape[3], pages.shape[0]
+    c, o = _describe_cache(pool, pages, D, dev), _describe_opts(scale, True, window, sinks, D)
+    _check_ints(kv_len, "kv_len", n, dev)
+    _check_ints(q_len, "q_len", n, dev)
+    if kv_max is None:
+        kv_max = c.max_pages * c.page_tokens
+    need = _U64()
+    fluid._check(_lib().fluid_kv_attention_workspace(_addr(c), _addr(o), kv_max, _addr(qd), C.byref(need)))
+    return (_lib(), dev, _addr(c), _addr(o), kv_max, _addr(qd), _addr(od), need.value, (c, o, qd, od))
 
 
 def kv_attention_workspace(pool, pages, q, kv_max=None, scale=None, window=0, sinks=0):
     """Bytes of workspace that ``kv_attention`` needs for these arguments."""
-    dev = pool.device
-    D = q.shape[3]
-    c, o, qd = _cache(pool, pages, D), _opts(scale, True, window, sinks, D), _tokens(q, "q", dev)
-    if kv_max is None:
-        kv_max = pages.shape[1] * (pool.shape[2] * 4 // (5 * D))
-    n = _U64()
-    fluid._check(_lib().fluid_kv_attention_workspace(c, o, kv_max, qd, C.byref(n)))
-    return n.value
+    return _kv_call(pool, pages, q, None, None, kv_max, scale, window, sinks, None)[7]
 
 
 def kv_attention(pool, pages, q, kv_len, q_len=None, kv_max=None, scale=None, window=0, sinks=0, out=None,
@@ -233,25 +260,47 @@ def kv_attention(pool, pages, q, kv_len, q_len=None, kv_max=None, scale=None, wi
     expect, which sizes the split of long caches over the GPU (by default all
     that a row of the table can name).  out: where to write (rows past q_len
     are left as they are; allocated as zeros by default).  Returns out."""
-    dev = _on_gpu(pool, "pool")
-    qd, D, n = _tokens(q, "q", dev), q.shape[3], pages.shape[0]
-    c, o = _cache(pool, pages, D), _opts(scale, True, window, sinks, D)
-    if kv_max is None:
-        kv_max = pages.shape[1] * (pool.shape[2] * 4 // (5 * D))
     if out is None:
-        out = _torch().zeros_like(q, memory_format=_torch().contiguous_format)
-    od = _tokens(out, "out", dev)
-    lib = _lib()
-    need = _U64()
-    fluid._check(lib.fluid_kv_attention_workspace(c, o, kv_max, qd, C.byref(need)))
-    keep, ws, ws_bytes = _workspace(need.value, workspace, dev, stream)
-    if kv_len is None:
-        _refuse("kv_len: needed")
-    fluid._check(lib.fluid_kv_attention(
-        c, pool.data_ptr(), pages.data_ptr(), o, kv_max, qd, q.data_ptr(), _ints(q_len, "q_len", n, dev),
-        _ints(kv_len, "kv_len", n, dev), od, out.data_ptr(), ws, ws_bytes, _stream(stream, dev)))
+        out = _zeros(q, stream)
+    key = (fluid._lib, pool.shape, pool.dtype, pool.get_device(), _form(pages), _form(q), _form(kv_len), _form(q_len),
+           kv_max, scale, window, sinks, _form(out))
+    made = _calls.get(key)
+    if made is None:
+        if kv_len is None:
+            _refuse("kv_len: needed")
+        made = _keep(key, _kv_call(pool, pages, q, kv_len, q_len, kv_max, scale, window, sinks, out))
+    lib, dev, c, o, kv_max, qd, od, need, _ = made
+    keep, ws, ws_bytes = _workspace(need, workspace, dev, stream) if need else (None, None, 0)
+    st = lib.fluid_kv_attention(
+        c, pool.data_ptr(), pages.data_ptr(), o, kv_max, qd, q.data_ptr(), None if q_len is None else q_len.data_ptr(),
+        kv_len.data_ptr(), od, out.data_ptr(), ws, ws_bytes, _raw_stream(dev) if stream is None else _stream(stream, dev))
     del keep
+    if st:
+        fluid._check(st)
     return out
+
+
+def _zeros(q, stream):
+    """Zeros of q's shape, filled on the call's stream."""
+    torch = _torch()
+    if stream is None or not q.is_cuda:
+        return torch.zeros(q.shape, dtype=q.dtype, device=q.device)
+    s = stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(stream, device=q.device)
+    with torch.cuda.stream(s):
+        return torch.zeros(q.shape, dtype=q.dtype, device=q.device)
+
+
+def _dense_call(q, k, v, q_len, kv_len, scale, causal, window, sinks, out):
+    dev = _device_of(q, "q")
+    qd, kd, vd = _describe(q, "q", dev), _describe(k, "k", dev), _describe(v, "v", dev)
+    od = _describe(out, "out", dev)
+    B, D = q.shape[0], q.shape[3]
+    o = _describe_opts(scale, causal, window, sinks, D)
+    _check_ints(q_len, "q_len", B, dev)
+    _check_ints(kv_len, "kv_len", B, dev)
+    need = _U64()
+    fluid._check(_lib().fluid_attention_workspace(_addr(o), _addr(qd), _addr(kd), C.byref(need)))
+    return (_lib(), dev, _addr(o), _addr(qd), _addr(kd), _addr(vd), _addr(od), need.value, (o, qd, kd, vd, od))
 
 
 def attention(q, k, v, q_len=None, kv_len=None, scale=None, causal=True, window=0, sinks=0, out=None,
@@ -264,21 +313,21 @@ def attention(q, k, v, q_len=None, kv_len=None, scale=None, causal=True, window=
     than ``window`` from its own (up to its own if causal) and the first
     ``sinks`` ones.  Rows that see nothing are zeros.  Returns out, as
     ``kv_attention`` does."""
-    dev = _on_gpu(q, "q")
-    qd, kd, vd = _tokens(q, "q", dev), _tokens(k, "k", dev), _tokens(v, "v", dev)
-    B, D = q.shape[0], q.shape[3]
-    o = _opts(scale, causal, window, sinks, D)
     if out is None:
-        out = _torch().zeros_like(q, memory_format=_torch().contiguous_format)
-    od = _tokens(out, "out", dev)
-    lib = _lib()
-    need = _U64()
-    fluid._check(lib.fluid_attention_workspace(o, qd, kd, C.byref(need)))
-    keep, ws, ws_bytes = _workspace(need.value, workspace, dev, stream)
-    fluid._check(lib.fluid_attention(
-        o, qd, q.data_ptr(), kd, k.data_ptr(), vd, v.data_ptr(), _ints(q_len, "q_len", B, dev),
-        _ints(kv_len, "kv_len", B, dev), od, out.data_ptr(), ws, ws_bytes, _stream(stream, dev)))
+        out = _zeros(q, stream)
+    key = (fluid._lib, _form(q), _form(k), _form(v), _form(q_len), _form(kv_len), scale, causal, window, sinks, _form(out))
+    made = _calls.get(key)
+    if made is None:
+        made = _keep(key, _dense_call(q, k, v, q_len, kv_len, scale, causal, window, sinks, out))
+    lib, dev, o, qd, kd, vd, od, need, _ = made
+    keep, ws, ws_bytes = _workspace(need, workspace, dev, stream) if need else (None, None, 0)
+    st = lib.fluid_attention(
+        o, qd, q.data_ptr(), kd, k.data_ptr(), vd, v.data_ptr(), None if q_len is None else q_len.data_ptr(),
+        None if kv_len is None else kv_len.data_ptr(), od, out.data_ptr(), ws, ws_bytes,
+        _raw_stream(dev) if stream is None else _stream(stream, dev))
     del keep
+    if st:
+        fluid._check(st)
     return out
 
 

@@ -158,32 +158,31 @@ def test_pool_bytes():
 def test_binding_refuses_tensors_that_cannot_be_right():
     torch = pytest.importorskip("torch")
     cpu = torch.zeros(1, 4, 2, 64)
-    with pytest.raises(F.FluidError, match="GPU"):
-        A.attention(cpu, cpu, cpu)
-    dev = cpu.device
-    with pytest.raises(F.FluidError, match="dimensions"):
-        A._tokens(cpu[0], "q", dev)
-    with pytest.raises(F.FluidError, match="dtype"):
-        A._tokens(cpu.half(), "q", dev)
-    with pytest.raises(F.FluidError, match="contiguous"):
-        A._tokens(cpu.transpose(2, 3), "q", dev)
-    with pytest.raises(F.FluidError, match="int32"):
-        A._ints(torch.zeros(2, dtype=torch.int64), "start", 2, dev)
-    with pytest.raises(F.FluidError, match="int32"):
-        A._ints(torch.zeros(3, dtype=torch.int32), "start", 2, dev)
     pages = torch.zeros(1, 2, dtype=torch.int32)
-    with pytest.raises(F.FluidError, match="block"):
-        A._cache(torch.zeros(2, 2, 100, dtype=torch.uint8), pages, 64)
-    with pytest.raises(F.FluidError, match="pool"):
-        A._cache(torch.zeros(2, 200, dtype=torch.uint8), pages, 64)
-    with pytest.raises(F.FluidError, match="pages"):
-        A._cache(torch.zeros(2, 2, 5120, dtype=torch.uint8), pages.long(), 64)
-    with pytest.raises(F.FluidError, match="window"):
-        A._opts(None, True, -1, 0, 64)
-    with pytest.raises(F.FluidError, match="scale"):
-        n = C.c_uint64()
-        F._check(A._lib().fluid_kv_attention_workspace(ref(cache()), A._opts(0.0, True, 0, 0, 64), 10, ref(tokens()),
-                                                       C.byref(n)))
+    pool = torch.zeros(2, 2, A.pool_block(32, 64), dtype=torch.uint8)
+    one = torch.zeros(1, dtype=torch.int32)
+    for call in (lambda: A.attention(cpu, cpu, cpu), lambda: A.kv_write(pool, pages, cpu, cpu, one),
+                 lambda: A.kv_read(pool, pages, one, cpu, cpu), lambda: A.kv_attention(pool, pages, cpu, one)):
+        with pytest.raises(F.FluidError, match="GPU"):
+            call()
+    dev = cpu.get_device()
+    for bad, word in ((cpu[0], "dimensions"), (cpu.half(), "dtype"), (cpu.transpose(2, 3), "contiguous")):
+        with pytest.raises(F.FluidError, match=word):
+            A._describe(bad, "q", dev)
+    with pytest.raises(F.FluidError, match="not on GPU 3"):
+        A._describe(cpu, "q", 3)
+    for bad in (torch.zeros(2, dtype=torch.int64), torch.zeros(3, dtype=torch.int32), torch.zeros(2, 1, dtype=torch.int32),
+                torch.zeros(4, dtype=torch.int32)[::2]):
+        with pytest.raises(F.FluidError, match="int32"):
+            A._check_ints(bad, "start", 2, dev)
+    for bad_pool, bad_pages, word in ((torch.zeros(2, 2, 100, dtype=torch.uint8), pages, "block"),
+                                      (torch.zeros(2, 200, dtype=torch.uint8), pages, "pool"), (pool.float(), pages, "pool"),
+                                      (pool, pages.long(), "pages"), (pool, pages[0], "pages")):
+        with pytest.raises(F.FluidError, match=word):
+            A._describe_cache(bad_pool, bad_pages, 64, dev)
+    for window, sinks, word in ((-1, 0, "window"), (0, -1, "sinks"), (1 << 31, 0, "window")):
+        with pytest.raises(F.FluidError, match=word):
+            A._describe_opts(None, True, window, sinks, 64)
 
 
 # ------------------------------------------------------- pins of the oracle
