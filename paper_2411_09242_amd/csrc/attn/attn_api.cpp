@@ -88,9 +88,12 @@ void kv_io(const fluid_kv_cache* cache, const void* pool, const int32_t* pages, 
   p.start = start;
   p.count = count;
   p.tokens = kd->tokens;
-  p.octets = (kd->tokens + 6) / 8 + 1;
-  p.items = int64_t(cache->batch) * p.octets * cache->kv_heads;
-  require(p.items * (cache->head_dim / 16) / 8 < kMostGroups, "k, v: too large for one launch");
+  const int span = write ? 8 : kKvTile;
+  p.runs = (kd->tokens + span - 2) / span + 1;
+  p.items = int64_t(cache->batch) * p.runs * cache->kv_heads;
+  require(p.items < kMostGroups, "k, v: too large for one launch");
+  p.div_heads = make_fastdiv(cache->kv_heads);
+  p.div_runs = make_fastdiv(p.runs);
   run_kv_io(p, kd->dtype, cache->head_dim, write, stream);
 }
 

@@ -17,7 +17,7 @@
 //
 // The wavefronts of a workgroup take token tiles in turn and join their sums
 // in LDS; long caches are split over workgroups, joined by a second kernel.
-#include "dev_attn.h"
+#include "kv_tile.h"
 #include "launch_attn.h"
 
 namespace fluid {
@@ -41,54 +41,6 @@ __device__ __forceinline__ float col_sum(float v) {
   v += __shfl_xor(v, 16);
   return v + __shfl_xor(v, 32);
 }
-
-template <int N>
-__device__ __forceinline__ void load_words(const uint8_t* p, uint32_t w[N]) {
-  typedef uint32_t vec __attribute__((ext_vector_type(N)));
-  if constexpr (N == 1) {
-    w[0] = __builtin_nontemporal_load((const uint32_t*)p);
-  } else {
-    const vec v = __builtin_nontemporal_load((const vec*)p);
-#pragma unroll
-    for (int i = 0; i < N; ++i) w[i] = v[i];
-  }
-}
-
-// The cache's words of one tile that a lane needs.
-template <int D>
-struct KvTile {
-  static constexpr int G = D / 32, WPL = D == 32 ? 2 : 4, NC = D == 32 ? 1 : D / 64;
-  uint32_t kw[2][G], kp[2][G];
-  uint32_t vw[NC][WPL], vs[NC][4], vb[NC][4];
-
-  // blk, P and slot are the same for all lanes; what a lane adds to the four
-  // parts' starts is not, but the same for every tile
-  struct Lane { uint32_t k, kp, v, vp; };
-  __device__ static __forceinline__ Lane lane_offsets(int lane) {
-    const int m = lane & 15, g = lane >> 4, t = 8 * (m >> 2) + (m & 3);
-    return {(uint32_t)(t * (D / 2) + g * (4 * G)), (uint32_t)(t * (4 * G)), (uint32_t)(g * (4 * D) + 4 * WPL * m),
-            (uint32_t)(g * (32 * G) + (D == 32 ? 0 : 32 * (m >> 3)))};
-  }
-  __device__ __forceinline__ void load_k(const uint8_t* blk, int P, int slot, const Lane& at) {
-    const uint8_t* const k = blk + slot * (D / 2);
-    const uint8_t* const kpairs = blk + P * (D / 2) + slot * (4 * G);
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      load_words<G>(k + at.k + 4 * i * (D / 2), kw[i]);
-      load_words<G>(kpairs + at.kp + 4 * i * (4 * G), kp[i]);
-    }
-  }
-  __device__ __forceinline__ void load_v(const uint8_t* blk, int P, int slot, const Lane& at) {
-    const uint8_t* const v = blk + P * (D / 2 + 4 * G) + slot * (D / 2);
-    const uint8_t* const vpairs = blk + P * (D + 4 * G) + slot * (4 * G);
-#pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      load_words<WPL>(v + at.v + 256 * c, vw[c]);
-      load_words<4>(vpairs + at.vp + 64 * c, vs[c]);
-      load_words<4>(vpairs + at.vp + 64 * c + 16, vb[c]);
-    }
-  }
-};
 
 // Whether the low f16 of w is an infinity or a NaN.
 __device__ __forceinline__ uint32_t odd_half(uint32_t w) { return (w & 0x7c00u) == 0x7c00u; }

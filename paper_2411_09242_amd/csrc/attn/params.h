@@ -30,8 +30,9 @@ struct KvIoParams {
   const int32_t* start;
   const int32_t* count;
   int32_t tokens;
-  int32_t octets;  // octets of tokens that T rows at any start can touch
-  int64_t items;   // batch * octets * kv_heads
+  int32_t runs;    // runs of 8 (write) or 32 (read) tokens that T rows at any start can touch
+  int64_t items;   // batch * runs * kv_heads, a wavefront each
+  FastDiv div_heads, div_runs;
 };
 
 // Rows are the (query, head of the group) pairs of one kv head, query slowest.

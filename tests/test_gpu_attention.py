@@ -119,6 +119,21 @@ def test_write_makes_the_formats_bytes_and_read_gives_their_values(dtype, D, P, 
             assert (host(got)[b, i, h] == host(torch.tensor(w).to(DT[dtype]))).all()
 
 
+def test_every_group_of_many_is_rounded_as_the_format_says():
+    """Pairs that one rounding more or less changes are one group in thousands."""
+    T, H, D = 2048, 16, 128
+    for dtype in ("f32", "bf16"):
+        k = rand(1, 1, T, H, D) * torch.exp(2 * rand(3, 1, T, H, 1)) + rand(4, 1, 1, H, D)
+        v = rand(2, 1, T, H, D).abs() * 100
+        k, v = k.to(DT[dtype]), v.to(DT[dtype])
+        pg = Paged([T], H, D, 256)
+        A.kv_write(pg.pool, pg.pages, k, v, ints([0]))
+        ko, vo = torch.empty(1, T, H, D, device="cuda"), torch.empty(1, T, H, D, device="cuda")
+        A.kv_read(pg.pool, pg.pages, ints([0]), ko, vo)
+        for x, got in ((k, ko), (v, vo)):
+            assert (host(got) == OA.values(*OA.quantise(host(x).astype(np.float32)))).all()
+
+
 @pytest.mark.parametrize("D", [32, 64, 128])
 def test_token_by_token_writes_the_bytes_of_one_call(D):
     k, v = rand(3, 1, 45, 2, D, dtype="bf16"), rand(4, 1, 45, 2, D, dtype="bf16")
