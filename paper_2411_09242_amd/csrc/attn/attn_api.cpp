@@ -180,9 +180,11 @@ AttnParams plan_attention(const fluid_attention_opts* opts, const fluid_tokens* 
           "q and k must have one dtype, batch and head_dim");
   p.kv_tokens = kd->tokens;
   p.row_tile = 128;
-  p.token_tile = qd->dtype == FLUID_BF16 ? 64 : 32;
+  p.token_tile = qd->dtype == FLUID_BF16 ? kBf16Tile : kF32Tile;
   const int64_t visible = visible_of(p, p.kv_tokens, std::min(p.q_tokens, p.row_tile / p.group + 1));
   plan_shares(p, visible, 128, 4);
+  p.by_xcd = int64_t(p.batch) * p.kv_heads % 8 == 0;
+  p.div_head = make_fastdiv(p.row_tiles * p.splits);
   return p;
 }
 

@@ -227,6 +227,13 @@ struct Share {
   }
   // false: nothing to do
   __device__ __forceinline__ bool find(const AttnParams& p, int block) {
+    // Workgroups go to the eight XCDs, which have an L2 each, in turn.  Heads
+    // are dealt to them likewise, so that a head's keys are read into one L2
+    // and the sequences of a ragged batch are spread over all.
+    if (p.by_xcd) {
+      const int j = block >> 3, head = (int)fdiv(j, p.div_head), of = p.row_tiles * p.splits;
+      block = ((block & 7) + 8 * head) * of + (j - head * of);
+    }
     index = (int)fdiv(block, p.div_splits);
     split = block - index * p.splits;
     const int x = (int)fdiv(index, p.div_tiles), b = (int)fdiv(x, p.div_heads);

@@ -18,6 +18,7 @@ namespace {
 
 typedef short v8i16 __attribute__((ext_vector_type(8)));
 typedef short v4i16 __attribute__((ext_vector_type(4)));
+typedef short s16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t piece __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) v4i16 lds_v4i16;
@@ -31,7 +32,7 @@ constexpr float kSlack = 8.0f;
 template <typename T, int D>
 struct Shape {
   static constexpr bool kBf16 = sizeof(T) == 2;
-  static constexpr int BN = kBf16 ? 64 : 32;       // tokens of a tile
+  static constexpr int BN = kBf16 ? kBf16Tile : kF32Tile;
   static constexpr int EPP = 16 / sizeof(T);       // elements of a 16-byte piece
   static constexpr int PPR = D / EPP;              // pieces of a token
   static constexpr int NP = BN * PPR / kThreads;   // pieces a thread moves, of K and of V
@@ -39,7 +40,7 @@ struct Shape {
   // Piece c of token t lies at place c ^ x(t) of its row, so that reads of
   // equal pieces of eight tokens (K), of equal 64-byte runs of four tokens
   // (bf16 V) or of tokens t and t + 4 (fp32 V) hit different banks.
-  __device__ static __forceinline__ int kx(int t) { return PPR == 4 ? (t >> 1) & 3 : t & 7; }
+  __device__ static __forceinline__ int kx(int t) { return PPR >= 16 ? t & 15 : (t / (16 / PPR)) & (PPR - 1); }
   __device__ static __forceinline__ int vx(int t) {
     if (kBf16) return D == 128 ? 4 * (t & 3) : D == 64 ? 4 * ((t >> 1) & 1) : 0;
     return PPR >= 16 ? 8 * ((t >> 2) & 1) : 0;
@@ -121,8 +122,8 @@ void attention_kernel(AttnParams p) {
       const int at = tid + kThreads * i, t = at / PPR, c = at % PPR, row = min(t, last);
       if constexpr (VEC) {
         const int to = EPP * (kThreads * i + 64 * wave);
-        copy_to_lds(k0 + (uint32_t)(row * (int)p.k.st + EPP * (c ^ S::kx(t))), sk + to);
-        copy_to_lds(v0 + (uint32_t)(row * (int)p.v.st + EPP * (c ^ S::vx(t))), sv + to);
+        copy_to_lds((const char*)k0 + (uint32_t)((row * (int)p.k.st + EPP * (c ^ S::kx(t))) * (int)sizeof(T)), sk + to);
+        copy_to_lds((const char*)v0 + (uint32_t)((row * (int)p.v.st + EPP * (c ^ S::vx(t))) * (int)sizeof(T)), sv + to);
       } else {
 #pragma unroll
         for (int e = 0; e < EPP; ++e) {
@@ -140,46 +141,58 @@ void attention_kernel(AttnParams p) {
 #pragma unroll
   for (int c = 0; c < CT; ++c) acc[c] = f32x16{};
 
-  // Weight 0 times a value that is no number would still be none.  Where
-  // rows differ in what they see and a value is infinite or NaN, such values
-  // are added to the sums of the rows that see them and become zeros in LDS.
-  auto part_odd = [&](int t0, T* sv) {
-    bool odd = false;
+  // whether all rows from position a to z see every token from t0 on of a tile
+  auto whole_for = [&](int t0, int a, int z) {
+    const int t1 = t0 + BN;
+    return t1 <= n && (!p.causal || t1 - 1 <= a) &&
+           (p.window <= 0 || t1 <= p.sinks || (t0 > z - p.window && (p.causal || t1 <= a + p.window)));
+  };
+  // Weight 0 times a value that is no number would still be none.  Where rows
+  // differ in what they see, such values become zeros in LDS, and the rows that
+  // do see them get them added at the end.
+  uint32_t dirty = 0;
+  auto clean = [&](T* sv) {
+#pragma nounroll
+    for (int at = tid; at < (BN * PPR); at += kThreads) {
+      piece w = *(const piece*)(sv + EPP * at), keep;
 #pragma unroll
-    for (int i = 0; i < NP; ++i)
-#pragma unroll
-      for (int e = 0; e < EPP; ++e) odd |= odd_value(Elem<T>::load(sv, (tid + kThreads * i) * EPP + e));
-    if (__builtin_expect(!__syncthreads_or(odd), 1)) return;
-    for (int t = 0; t < BN && live; ++t) {
-      if (!eye.sees(t0 + t)) continue;
-#pragma unroll
-      for (int c = 0; c < CT; ++c)
-#pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          const int e = 32 * c + 8 * (v >> 2) + 4 * half + (v & 3);
-          const float x = Elem<T>::load(sv, S::v(t, e / EPP) + e % EPP);
-          if (odd_value(x)) acc[c][v] += x;
-        }
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (kBf16)
+          keep[i] = ((w[i] & 0x7f80u) == 0x7f80u ? 0u : 0xffffu) | ((w[i] & 0x7f800000u) == 0x7f800000u ? 0u : 0xffff0000u);
+        else
+          keep[i] = (w[i] & 0x7f800000u) == 0x7f800000u ? 0u : 0xffffffffu;
+      }
+      const uint32_t odd = ~(keep[0] & keep[1] & keep[2] & keep[3]);
+      if (odd) *(piece*)(sv + EPP * at) = w & keep;
+      dirty |= odd;
     }
     __syncthreads();
-    for (int i = 0; i < NP * EPP; ++i) {
-      const int at = (tid + kThreads * (i / EPP)) * EPP + i % EPP;
-      if (odd_value(Elem<T>::load(sv, at))) sv[at] = 0;
+  };
+  auto add_odd = [&]() {
+#pragma nounroll
+    for (int u = u0; u < u1; ++u) {
+      const int t0 = range.tile(u) * BN;
+      if (whole_for(t0, bp_min, bp_max)) continue;
+#pragma nounroll
+      for (int t = t0; t < min(t0 + BN, n); ++t) {
+        if (!eye.sees(t)) continue;
+#pragma unroll
+        for (int c = 0; c < CT; ++c)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) {
+            const float x = Elem<T>::load(vb, t * p.v.st + 32 * c + 8 * (v >> 2) + 4 * half + (v & 3));
+            if (odd_value(x)) acc[c][v] += x;
+          }
+      }
     }
-    __syncthreads();
   };
 
   auto step = [&](int u, T* sk, T* sv, T* next_k, T* next_v) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
+    const int t0 = range.tile(u) * BN;
+    if (!whole_for(t0, bp_min, bp_max)) clean(sv);
     if (u + 1 < u1) stage(u + 1, next_k, next_v);
-    const int t0 = range.tile(u) * BN, t1 = t0 + BN;
-    // whether all rows from position a to b see every token of the tile
-    auto whole_for = [&](int a, int z) {
-      return t1 <= n && (!p.causal || t1 - 1 <= a) &&
-             (p.window <= 0 || t1 <= p.sinks || (t0 > z - p.window && (p.causal || t1 <= a + p.window)));
-    };
-    if (!whole_for(bp_min, bp_max)) part_odd(t0, sv);
     if (!live) return;
     f32x16 s[NT];
 #pragma unroll
@@ -200,7 +213,7 @@ void attention_kernel(AttnParams p) {
         }
       }
     }
-    if (!whole_for(wp_min, wp_max)) {
+    if (!whole_for(t0, wp_min, wp_max)) {
 #pragma unroll
       for (int i = 0; i < NT; ++i)
 #pragma unroll
@@ -226,21 +239,25 @@ void attention_kernel(AttnParams p) {
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
         s[i][v] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i][v], p.cs, -m));
-        l += s[i][v];
+        if constexpr (!kBf16) l += s[i][v];
       }
     if constexpr (kBf16) {
       bf16x8 pr[2 * NT];  // part c: tokens 16 c + 8 (e / 4) + 4 half + e % 4
 #pragma unroll
       for (int c = 0; c < 2 * NT; ++c)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) pr[c][e] = (__bf16)s[c >> 1][8 * (c & 1) + e];
+        for (int e = 0; e < 8; e += 2) {
+          const bf16x2 w = __builtin_convertvector(f32x2{s[c >> 1][8 * (c & 1) + e], s[c >> 1][8 * (c & 1) + e + 1]}, bf16x2);
+          l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(s16x2, w), s16x2{0x3f80, 0x3f80}, l, false);
+          pr[c][e] = w[0], pr[c][e + 1] = w[1];
+        }
       // this lane's source of a transposing read: one token of four, four
       // channels of sixteen
       const int tr = 4 * half + ((lane & 15) >> 2), ch = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
 #pragma unroll
-      for (int c = 0; c < CT; ++c)
+      for (int k = 0; k < 2 * NT; ++k)
 #pragma unroll
-        for (int k = 0; k < 2 * NT; ++k) {
+        for (int c = 0; c < CT; ++c) {
           auto at = [&](int t) { return (lds_v4i16*)(sv + S::v(t, (32 * c + ch) >> 3) + (ch & 7)); };
           const v4i16 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(at(16 * k + tr));
           const v4i16 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(at(16 * k + 8 + tr));
@@ -264,6 +281,7 @@ void attention_kernel(AttnParams p) {
     if (u + 1 < u1) step(u + 1, sk1, sv1, sk0, sv0);
   }
 
+  if (__syncthreads_or(dirty) && live) add_odd();
   if (live && w0 + col < r1) {
     l += __shfl_xor(l, 32);
     if (!sh.whole()) {

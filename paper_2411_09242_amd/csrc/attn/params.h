@@ -49,9 +49,12 @@ struct AttnParams {
   int32_t splits;  // most shares of an item, a workgroup each
   int32_t chunk;   // steps of a share
   FastDiv div_group, div_tiles, div_heads, div_splits;
+  int32_t by_xcd;     // 1: a kv head's workgroups on one XCD
+  FastDiv div_head;   // by a kv head's workgroups
   float* ws;       // splits > 1: [item][split] of row_tile maxima, sums and rows of partial sums
 };
 
-constexpr int kKvTile = 32;  // tokens of a step over the 4-bit cache
+// tokens of a step over the 4-bit cache, and over bf16 and fp32 keys and values
+constexpr int kKvTile = 32, kBf16Tile = 64, kF32Tile = 32;
 
 }  // namespace fluid
