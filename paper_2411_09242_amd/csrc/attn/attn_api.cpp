@@ -98,12 +98,15 @@ void kv_io(const fluid_kv_cache* cache, const void* pool, const int32_t* pages, 
 }
 
 // How an attention is cut into workgroups: items (a tile of rows of one kv
-// head) times splits, which share the item's steps (tiles of tokens).
-void plan_shares(AttnParams& p, int64_t visible, int64_t target, int64_t least) {
+// head) times splits, which share the item's steps (tiles of tokens): as many
+// as make `slots` workgroups in all, the number that the GPU runs at once, but
+// shares of at least `least` steps.
+void plan_shares(AttnParams& p, int64_t visible, int64_t slots, int64_t least) {
   p.row_tiles = (int32_t)((int64_t(p.q_tokens) * p.group + p.row_tile - 1) / p.row_tile);
   const int64_t items = int64_t(p.batch) * p.kv_heads * p.row_tiles;
   const int64_t steps = visible / p.token_tile + 1;
-  int64_t splits = std::max<int64_t>(1, std::min((target + items - 1) / items, steps / least));
+  // a row's shares are put together by one workgroup: 507 of them took 4 us more than 254
+  const int64_t splits = std::max<int64_t>(1, std::min({slots / items, steps / least, (int64_t)256}));
   p.chunk = (int32_t)((steps + splits - 1) / splits);
   p.splits = (int32_t)((steps + p.chunk - 1) / p.chunk);
   require(items * p.splits < kMostGroups && int64_t(p.batch) * p.kv_heads * p.q_tokens * p.group < kMostGroups,
@@ -168,10 +171,12 @@ AttnParams plan_kv_attention(const fluid_kv_cache* cache, const fluid_attention_
   p.token_tile = kKvTile;
   const int64_t visible =
       visible_of(p, std::min(kv_max, p.kv_tokens), std::min(p.q_tokens, p.row_tile / p.group + 1));
-  // three workgroups to a compute unit, one round of them: 131072 tokens of
+  // one round of the three workgroups that fit a compute unit: 131072 tokens of
   // 8 heads take 42.8 us with 768 workgroups, 47.1 with twice and 53.7 with
-  // three times as many; a share of at least 8 steps, two to a wavefront
-  plan_shares(p, visible, 768, 8);
+  // three times as many; 16 sequences of 1000 tokens and 32 heads 18.5 us with
+  // 512 and 24.9 with 1024.  With 32 rows to a workgroup two fit, and one is as
+  // fast (16000 tokens of 16 heads, 16 rows each: 20.7 us, 23.5 with two).
+  plan_shares(p, visible, p.row_tile == 16 ? 768 : 256, 8);
   return p;
 }
 AttnParams plan_attention(const fluid_attention_opts* opts, const fluid_tokens* qd, const fluid_tokens* kd) {
@@ -182,7 +187,12 @@ AttnParams plan_attention(const fluid_attention_opts* opts, const fluid_tokens* 
   p.row_tile = 128;
   p.token_tile = qd->dtype == FLUID_BF16 ? kBf16Tile : kF32Tile;
   const int64_t visible = visible_of(p, p.kv_tokens, std::min(p.q_tokens, p.row_tile / p.group + 1));
-  plan_shares(p, visible, 128, 4);
+  // The shares of many rows are not worth putting together: four second chunks
+  // of 333 tokens (21312 rows) take 20 us in 176 workgroups, and 53 in 352 with
+  // the join.  One token of 8 sequences over 4096 (256 rows): 62 us in 128
+  // workgroups, 33 in 512.
+  const bool few = int64_t(p.batch) * p.q_tokens * qd->heads <= 8192;
+  plan_shares(p, visible, few ? 512 : 1, 2);
   p.by_xcd = int64_t(p.batch) * p.kv_heads % 8 == 0;
   p.div_head = make_fastdiv(p.row_tiles * p.splits);
   return p;
