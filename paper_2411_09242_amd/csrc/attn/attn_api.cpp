@@ -193,6 +193,10 @@ AttnParams plan_attention(const fluid_attention_opts* opts, const fluid_tokens* 
   // workgroups, 33 in 512.
   const bool few = int64_t(p.batch) * p.q_tokens * qd->heads <= 8192;
   plan_shares(p, visible, few ? 512 : 1, 2);
+  // Two teams where that still is one round of workgroups.  fp32 with 128
+  // channels has no room for a second team's stages.
+  const int64_t groups = int64_t(p.batch) * p.kv_heads * p.row_tiles * p.splits;
+  p.teams = groups <= 256 && !(qd->dtype == FLUID_F32 && qd->head_dim == 128) ? 2 : 1;
   p.by_xcd = int64_t(p.batch) * p.kv_heads % 8 == 0;
   p.div_head = make_fastdiv(p.row_tiles * p.splits);
   return p;

@@ -46,6 +46,7 @@ struct AttnParams {
   float cs;          // scale * log2(e)
   int32_t row_tile, token_tile;  // rows and tokens of a workgroup's step
   int32_t row_tiles;             // tiles of rows of one kv head
+  int32_t teams;   // attention: teams of four wavefronts to a workgroup
   int32_t splits;  // most shares of an item, a workgroup each
   int32_t chunk;   // steps of a share
   FastDiv div_group, div_tiles, div_heads, div_splits;
