@@ -177,6 +177,15 @@ AttnParams plan_kv_attention(const fluid_kv_cache* cache, const fluid_attention_
   // 512 and 24.9 with 1024.  With 32 rows to a workgroup two fit, and one is as
   // fast (16000 tokens of 16 heads, 16 rows each: 20.7 us, 23.5 with two).
   plan_shares(p, visible, p.row_tile == 16 ? 768 : 256, 8);
+  p.waves = 4;
+  // Few tokens are left to one larger workgroup, which saves the join: up to
+  // four steps to a wavefront.  1024 tokens of 32 heads of 128: 9.7 us in one
+  // launch, 12.5 in two; 2048 tokens 15.1 and 12.0.
+  const int many = kv_waves(qd->head_dim);
+  if (p.row_tile == 16 && p.splits > 1 && visible / p.token_tile < 4 * many) {
+    plan_shares(p, visible, 1, 1);
+    p.waves = many;
+  }
   return p;
 }
 AttnParams plan_attention(const fluid_attention_opts* opts, const fluid_tokens* qd, const fluid_tokens* kd) {

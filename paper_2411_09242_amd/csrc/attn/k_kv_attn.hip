@@ -45,17 +45,15 @@ __device__ __forceinline__ float col_sum(float v) {
 // Whether the low f16 of w is an infinity or a NaN.
 __device__ __forceinline__ uint32_t odd_half(uint32_t w) { return (w & 0x7c00u) == 0x7c00u; }
 
-constexpr int kWaves = 4;
-
-template <typename T, int D, int MT>
-__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(MT == 1 ? 3 : 2)))
+template <typename T, int D, int MT, int NW>
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NW == 16 ? 4 : MT == 1 && NW == 4 ? 3 : 2)))
 void kv_attention_kernel(AttnParams p) {
   constexpr bool kTwo = sizeof(T) == 4;  // operands in two f16 parts
   constexpr int G = D / 32, R = 16 * MT;
   using Tile = KvTile<D>;
   constexpr int WPL = Tile::WPL, NC = Tile::NC;
-  __shared__ float sh_m[kWaves][R], sh_l[kWaves][R];
-  __shared__ __attribute__((aligned(16))) float sh_o[kWaves][R][D + 4];
+  __shared__ float sh_m[NW][R], sh_l[NW][R];
+  __shared__ __attribute__((aligned(16))) float sh_o[NW][R][D + 4];
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, g4 = lane >> 4;
@@ -147,7 +145,7 @@ void kv_attention_kernel(AttnParams p) {
   // likewise: about half a tile is always on its way, in the same registers.
   while (u < u1) {
     const int t0 = range.tile(u) * kKvTile;
-    const int after = min(u + kWaves, u1 - 1), next = page_of(after);
+    const int after = min(u + NW, u1 - 1), next = page_of(after);
     const bool dark = (uint32_t)page >= (uint32_t)p.c.n_pages;
     // every row sees every token
     const bool whole = !dark && t0 + kKvTile - 1 <= p_min &&
@@ -258,7 +256,7 @@ void kv_attention_kernel(AttnParams p) {
         }
       }
     tile.load_v(block(next), P, slot(after), at);
-    u += kWaves;
+    u += NW;
     page = next;
   }
 
@@ -288,15 +286,15 @@ void kv_attention_kernel(AttnParams p) {
   }
   __syncthreads();
   constexpr int TPR = D / 8;  // threads a row
-  for (int k = threadIdx.x; k < R * TPR; k += 64 * kWaves) {
+  for (int k = threadIdx.x; k < R * TPR; k += 64 * NW) {
     const int r = k / TPR, c = 8 * (k - r * TPR);
     if (r0 + r >= r1) continue;
     float top = sh_m[0][r];
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) top = fmaxf(top, sh_m[w][r]);
+    for (int w = 1; w < NW; ++w) top = fmaxf(top, sh_m[w][r]);
     float sum = 0.0f, o[8] = {0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
+    for (int w = 0; w < NW; ++w) {
       const float a = __builtin_amdgcn_exp2f(sh_m[w][r] - top);
       sum += a * sh_l[w][r];
 #pragma unroll
@@ -320,21 +318,22 @@ void kv_attention_kernel(AttnParams p) {
   }
 }
 
+template <typename T, int D>
+hipError_t launch_dim(const AttnParams& p, hipStream_t s) {
+  constexpr int MANY = kv_waves(D);
+  const dim3 grid((uint32_t)((int64_t)p.batch * p.kv_heads * p.row_tiles * p.splits)), block(64 * p.waves);
+  if (p.row_tile == 32) hipLaunchKernelGGL((kv_attention_kernel<T, D, 2, 4>), grid, block, 0, s, p);
+  else if (p.waves == MANY) hipLaunchKernelGGL((kv_attention_kernel<T, D, 1, MANY>), grid, block, 0, s, p);
+  else hipLaunchKernelGGL((kv_attention_kernel<T, D, 1, 4>), grid, block, 0, s, p);
+  return hipGetLastError();
+}
 template <typename T>
 hipError_t launch(const AttnParams& p, int D, hipStream_t s) {
-  const dim3 grid((uint32_t)((int64_t)p.batch * p.kv_heads * p.row_tiles * p.splits)), block(64 * kWaves);
-#define FLUID_KV_D(N)                                                                                      \
-  case N:                                                                                                  \
-    if (p.row_tile == 16) hipLaunchKernelGGL((kv_attention_kernel<T, N, 1>), grid, block, 0, s, p);       \
-    else hipLaunchKernelGGL((kv_attention_kernel<T, N, 2>), grid, block, 0, s, p);                        \
-    break;
   switch (D) {
-    FLUID_KV_D(32)
-    FLUID_KV_D(64)
-    FLUID_KV_D(128)
+    case 32: return launch_dim<T, 32>(p, s);
+    case 64: return launch_dim<T, 64>(p, s);
+    default: return launch_dim<T, 128>(p, s);
   }
-#undef FLUID_KV_D
-  return hipGetLastError();
 }
 
 }  // namespace

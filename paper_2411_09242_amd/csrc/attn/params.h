@@ -46,6 +46,7 @@ struct AttnParams {
   float cs;          // scale * log2(e)
   int32_t row_tile, token_tile;  // rows and tokens of a workgroup's step
   int32_t row_tiles;             // tiles of rows of one kv head
+  int32_t waves;   // kv_attention: wavefronts of a workgroup
   int32_t teams;   // attention: teams of four wavefronts to a workgroup
   int32_t splits;  // most shares of an item, a workgroup each
   int32_t chunk;   // steps of a share
@@ -57,5 +58,9 @@ struct AttnParams {
 
 // tokens of a step over the 4-bit cache, and over bf16 and fp32 keys and values
 constexpr int kKvTile = 32, kBf16Tile = 64, kF32Tile = 32;
+
+// Wavefronts of a workgroup that has an item's tokens to itself: as many as the
+// registers of a compute unit hold.
+constexpr int kv_waves(int head_dim) { return head_dim == 128 ? 8 : 16; }
 
 }  // namespace fluid
