@@ -186,8 +186,9 @@ def _io_call(pool, pages, k, v, start, count):
 
 
 def _io(write, pool, pages, k, v, start, count, stream):
-    key = (fluid._lib, pool.shape, pool.dtype, pool.get_device(), _form(pages), _form(k), _form(v), _form(start),
-           _form(count))
+    key = (fluid._lib, pool.shape, pool.stride(), pool.dtype, pool.get_device(), pages.shape, pages.stride(), pages.dtype,
+           pages.get_device(), k.dtype, k.shape, k.stride(), k.get_device(), v.dtype, v.shape, v.stride(),
+           v.get_device(), _form(start), None if count is None else _form(count))
     made = _calls.get(key)
     if made is None:
         made = _keep(key, _io_call(pool, pages, k, v, start, count))
@@ -262,8 +263,9 @@ def kv_attention(pool, pages, q, kv_len, q_len=None, kv_max=None, scale=None, wi
     are left as they are; allocated as zeros by default).  Returns out."""
     if out is None:
         out = _zeros(q, stream)
-    key = (fluid._lib, pool.shape, pool.dtype, pool.get_device(), _form(pages), _form(q), _form(kv_len), _form(q_len),
-           kv_max, scale, window, sinks, _form(out))
+    key = (fluid._lib, pool.shape, pool.stride(), pool.dtype, pool.get_device(), pages.shape, pages.stride(), pages.dtype,
+           pages.get_device(), q.dtype, q.shape, q.stride(), q.get_device(), out.dtype, out.shape, out.stride(),
+           out.get_device(), _form(kv_len), None if q_len is None else _form(q_len), kv_max, scale, window, sinks)
     made = _calls.get(key)
     if made is None:
         if kv_len is None:
@@ -315,7 +317,10 @@ def attention(q, k, v, q_len=None, kv_len=None, scale=None, causal=True, window=
     ``kv_attention`` does."""
     if out is None:
         out = _zeros(q, stream)
-    key = (fluid._lib, _form(q), _form(k), _form(v), _form(q_len), _form(kv_len), scale, causal, window, sinks, _form(out))
+    key = (fluid._lib, q.dtype, q.shape, q.stride(), q.get_device(), k.dtype, k.shape, k.stride(), k.get_device(),
+           v.dtype, v.shape, v.stride(), v.get_device(), out.dtype, out.shape, out.stride(), out.get_device(),
+           None if q_len is None else _form(q_len), None if kv_len is None else _form(kv_len), scale, causal, window,
+           sinks)
     made = _calls.get(key)
     if made is None:
         made = _keep(key, _dense_call(q, k, v, q_len, kv_len, scale, causal, window, sinks, out))

@@ -499,3 +499,18 @@ def test_cache_object_grows_trims_and_refuses():
     c.clear(0)
     assert c.lengths == [0, 38] and len(c.free) == 7
     assert (c.attend(q)[0] == 0).all()
+
+
+def test_checks_hold_behind_a_call_of_the_same_shapes():
+    block = A.pool_block(32, 64)
+    pages, at, one = ints([0]).view(1, 1), ints([0]), ints([1])
+    k = rand(1, 1, 1, 2, 64, dtype="bf16")
+    pool = torch.zeros(2, 2, block, dtype=torch.uint8, device="cuda")
+    calls = (lambda p: A.kv_write(p, pages, k, k, at), lambda p: A.kv_read(p, pages, at, k.clone(), k.clone()),
+             lambda p: A.kv_attention(p, pages, k, one))
+    apart = pool.transpose(0, 1)[:1]
+    assert apart.shape == pool[:1].shape and not apart.is_contiguous()
+    for call in calls:
+        call(pool[:1])
+        with pytest.raises(F.FluidError, match="contiguous"):
+            call(apart)
