@@ -196,12 +196,13 @@ AttnParams plan_attention(const fluid_attention_opts* opts, const fluid_tokens* 
   p.row_tile = 128;
   p.token_tile = qd->dtype == FLUID_BF16 ? kBf16Tile : kF32Tile;
   const int64_t visible = visible_of(p, p.kv_tokens, std::min(p.q_tokens, p.row_tile / p.group + 1));
-  // The shares of many rows are not worth putting together: four second chunks
-  // of 333 tokens (21312 rows) take 20 us in 176 workgroups, and 53 in 352 with
-  // the join.  One token of 8 sequences over 4096 (256 rows): 62 us in 128
-  // workgroups, 33 in 512.
-  const bool few = int64_t(p.batch) * p.q_tokens * qd->heads <= 8192;
-  plan_shares(p, visible, few ? 512 : 1, 2);
+  // One round of workgroups, one to a compute unit.  512 queries of 32 heads
+  // behind 7680 tokens, bf16: 121 us in 128 workgroups, 80 in 256 or 512, 91 in
+  // 1024; 64 queries behind 4032: 64 us in 16, 19 in 256, 23 in 512; fp32: 437,
+  // 48 and 60.  A short bf16 loop is not worth a second launch: 512 queries of
+  // 12 heads over 512 tokens 11.2 us in one, 13.3 in two (fp32: 28.5 and 18.3).
+  const bool brief = qd->dtype == FLUID_BF16 && visible <= 512;
+  plan_shares(p, visible, brief ? 1 : 256, 2);
   // Two teams where that still is one round of workgroups.  fp32 with 128
   // channels has no room for a second team's stages.
   const int64_t groups = int64_t(p.batch) * p.kv_heads * p.row_tiles * p.splits;
