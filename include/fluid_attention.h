@@ -27,9 +27,8 @@ extern "C" {
 #endif
 
 /* A tensor of tokens.  Channels are contiguous; stride holds the distance in
- * elements between sequences, tokens and heads (any sign is refused but
- * positive or zero for inputs; outputs must not overlap themselves).  head_dim
- * is 32, 64 or 128.  Rows that start on 16-byte addresses are fastest; others
+ * elements between sequences, tokens and heads (not negative; 0 repeats an
+ * input, outputs must not overlap themselves).  head_dim is 32, 64 or 128.  Rows that start on 16-byte addresses are fastest; others
  * are read and written element by element. */
 typedef struct {
   int32_t dtype; /* FLUID_F32 or FLUID_BF16 */
@@ -64,8 +63,8 @@ typedef struct {
  * holds tokens i * page_tokens .. of the sequence.  An entry outside
  * [0, n_pages) holds no tokens: nothing is written to it, kv_read leaves its
  * rows as they are and attention does not see its tokens.  So a page that a
- * window has left behind can be given back.  A page written by one sequence
- * must not be in another's row. */
+ * window has left behind can be given back.  Sequences may share pages that
+ * are only read; a page that a call writes to must be in one row alone. */
 typedef struct {
   int32_t n_pages, page_tokens; /* page_tokens: 32, 64, 128, 256, 512 or 1024 */
   int32_t kv_heads, head_dim;   /* head_dim: 32, 64 or 128 */
@@ -130,7 +129,11 @@ fluid_status fluid_kv_attention(const fluid_kv_cache* cache, const void* pool, c
 /* Attention of q [batch, T, heads, head_dim] over k, v [batch, N, kv_heads,
  * head_dim], all of one dtype.  Lengths as above (NULL: T and N; kv_len is
  * clamped to [0, N]); rows of k and v from kv_len[b] on are not used.
- * Workspace and errors as fluid_kv_attention. */
+ * Arithmetic: on the bf16 matrix cores with fp32 sums, softmax in fp32.  bf16:
+ * a weight is rounded to bf16 for its product with the value, and so summed.
+ * fp32: operands are three bf16 parts each, which leaves the error of an fp32
+ * product; magnitudes from 3.3895e38 on, beyond bf16's largest, count as
+ * infinite.  Workspace and errors as fluid_kv_attention. */
 fluid_status fluid_attention_workspace(const fluid_attention_opts* opts, const fluid_tokens* qd,
                                        const fluid_tokens* kd, uint64_t* bytes);
 fluid_status fluid_attention(const fluid_attention_opts* opts, const fluid_tokens* qd, const void* q,

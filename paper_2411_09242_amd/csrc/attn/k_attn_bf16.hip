@@ -2,6 +2,15 @@
 // scores kept in registers (attn_rows.h).  Keys and values go from memory to
 // LDS without registers, one tile of 64 tokens ahead of the products; V is
 // read back by transposing reads.
+//
+// 8192 queries of 32 heads of 128 (8 of keys), window 2048: 270 us (300 on a
+// slower card), 890 TFLOP/s of the products needed, where a library product of
+// 8192^3 reaches 1140.  MFMA are 47 % and vector instructions 44 % of the
+// cycles, at a clock of 1.8 GHz of 2.4: power bounds it.  The products alone,
+// without copies and weights, take 193 us; with LDS operands read further
+// ahead, copies a step and a half ahead behind two barriers, or one of a
+// SIMD's two wavefronts preferred the time is the same or worse.  2048 queries
+// (window 1024) take 48 us, most of it the 18 steps of the longest rows.
 #include "attn_rows.h"
 #include "launch_attn.h"
 

@@ -5,10 +5,14 @@
 // each part what the ones before leave, rounded: 24 bits.  A product is summed
 // from the six of the nine products of parts that matter (h h, h m, m h, m m,
 // h l, l h); the three left out are together at most 2^-24 of it, an fp32
-// rounding.  Six products take 6/16 of the time of the fp32 MFMA for as much
-// (eight channels of 32x32x2 at 64 cycles against six times 16 channels at 32).
-// Keys and values are split on their way from memory through registers to LDS,
-// one tile of 32 tokens ahead of the products.
+// rounding.  For 16 channels these are six MFMAs of 32 cycles, where the fp32
+// MFMA needs eight of 64.  Keys and values are split on their way from memory
+// through registers to LDS, one tile of 32 tokens ahead of the products.
+//
+// 8 sequences of 207 to 512 tokens of 16 heads of 64, both directions: 42 us,
+// 61 with the fp32 MFMA.  Vector instructions (exponentials, splits of the
+// weights and of the keys and values that every workgroup loads) are 43 % of
+// the cycles, MFMA 36 %, and two wavefronts a SIMD do not hide all waits.
 #include "attn_rows.h"
 #include "launch_attn.h"
 
