@@ -28,8 +28,9 @@ extern "C" {
 
 /* A tensor of tokens.  Channels are contiguous; stride holds the distance in
  * elements between sequences, tokens and heads (not negative; 0 repeats an
- * input, outputs must not overlap themselves).  head_dim is 32, 64 or 128.  Rows that start on 16-byte addresses are fastest; others
- * are read and written element by element. */
+ * input; an output's are at least head_dim, and its elements must not
+ * overlap).  head_dim is 32, 64 or 128.  Rows that start on 16-byte addresses
+ * are fastest; others are read and written element by element. */
 typedef struct {
   int32_t dtype; /* FLUID_F32 or FLUID_BF16 */
   int32_t batch, tokens, heads, head_dim;

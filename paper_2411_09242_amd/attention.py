@@ -368,7 +368,12 @@ class KvCache:
     def append(self, k, v, counts=None):
         """Write tokens k, v [batch, T, kv_heads, head_dim] behind what every
         sequence holds (counts: how many of each, on the host)."""
-        counts = [k.shape[1]] * len(self.lengths) if counts is None else list(counts)
+        batch = len(self.lengths)
+        if k.dim() != 4 or k.shape[0] != batch:
+            _refuse(f"k: a tensor [{batch}, tokens, heads, head_dim] is needed, got {tuple(k.shape)}")
+        counts = [k.shape[1]] * batch if counts is None else list(counts)
+        if len(counts) != batch:
+            _refuse(f"counts: {batch} are needed, got {len(counts)}")
         start = list(self.lengths)
         for b, n in enumerate(counts):
             if not 0 <= n <= k.shape[1] or start[b] + n > self.max_tokens:
@@ -383,7 +388,15 @@ class KvCache:
         self.lengths = [s + n for s, n in zip(start, counts)]
         at = self.kv_len.clone()
         self._push()
-        kv_write(self.pool, self.pages, k, v, at, self.kv_len - at)
+        try:
+            kv_write(self.pool, self.pages, k, v, at, self.kv_len - at)
+        except Exception:  # nothing was written: as if not called
+            for b, i in reversed(new):
+                self.free.append(self.table[b][i])
+                self.table[b][i] = -1
+            self.lengths = start
+            self._push()
+            raise
 
     def attend(self, q, q_len=None, **kw):
         """``kv_attention`` of q over the cache."""
@@ -395,7 +408,12 @@ class KvCache:
         kv_read(self.pool, self.pages, self.torch.zeros_like(self.kv_len), k, v, self.kv_len)
 
     def trim(self, window, sinks=0):
-        """Give back the pages that no query from the newest token on sees."""
+        """Give back the pages that no query from the newest token on sees: none
+        without a window (0)."""
+        if window < 0 or sinks < 0:
+            _refuse(f"window, sinks: {window}, {sinks} must not be negative")
+        if window == 0:
+            return
         for b, n in enumerate(self.lengths):
             for i in range(max(0, n - window) // self.page_tokens):
                 if i * self.page_tokens >= sinks and self.table[b][i] >= 0:

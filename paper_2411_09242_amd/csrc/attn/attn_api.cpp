@@ -44,6 +44,15 @@ TokensArg tokens_data(const fluid_tokens* d, const void* p, const char* name) {
   return tokens_arg(d, p, name);
 }
 
+// Neighbours of an output must not share elements (equal strides of two
+// dimensions remain the caller's to avoid).
+void check_apart(const fluid_tokens* d, const char* name) {
+  const int32_t extent[3] = {d->batch, d->tokens, d->heads};
+  for (int i = 0; i < 3; ++i)
+    require(extent[i] == 1 || d->stride[i] >= d->head_dim,
+            std::string(name) + ": an output's strides must be at least head_dim");
+}
+
 int64_t block_bytes(const fluid_kv_cache* c) { return int64_t(5) * c->head_dim * c->page_tokens / 4; }
 
 KvArgs check_cache(const fluid_kv_cache* c) {
@@ -85,6 +94,10 @@ void kv_io(const fluid_kv_cache* cache, const void* pool, const int32_t* pages, 
   for (const fluid_tokens* d : {kd, vd})
     require(d->batch == cache->batch && d->heads == cache->kv_heads && d->head_dim == cache->head_dim,
             "k and v must have the cache's batch, kv_heads and head_dim");
+  if (!write) {
+    check_apart(kd, "k");
+    check_apart(vd, "v");
+  }
   p.start = start;
   p.count = count;
   p.tokens = kd->tokens;
@@ -260,6 +273,7 @@ fluid_status fluid_kv_attention(const fluid_kv_cache* cache, const void* pool, c
     check_out(qd, od);
     require(kv_len != nullptr, "kv_len: NULL");
     AttnParams p = plan_kv_attention(cache, opts, kv_max, qd);
+    check_apart(od, "out");
     p.c = c;
     p.q = qa;
     p.o = oa;
@@ -292,6 +306,7 @@ fluid_status fluid_attention(const fluid_attention_opts* opts, const fluid_token
                 kd->head_dim == vd->head_dim,
             "k and v must have one dtype and shape");
     AttnParams p = plan_attention(opts, qd, kd);
+    check_apart(od, "out");
     p.q = qa;
     p.k = ka;
     p.v = va;

@@ -129,6 +129,17 @@ def test_more_refusals():
         assert st == INVALID and word in msg, (st, msg)
 
 
+def test_outputs_that_repeat_elements_are_refused():
+    for stride in ((0, 128, 64), (640, 0, 64), (640, 128, 0), (640, 128, 32)):
+        kd = tokens(heads=2, stride=stride)
+        q = tokens(heads=2, stride=stride)
+        assert io(kd=kd, vd=kd)[0] == UNSUPPORTED  # as inputs they may
+        for st, msg in (io(kd=kd, write=False), io(vd=kd, write=False), kv(qd=q, od=q), dense(qd=q, od=q)):
+            assert st == INVALID and "head_dim" in msg, (stride, st, msg)
+    one = tokens(heads=2, batch=1, stride=(0, 128, 64))  # a stride that is never used
+    assert io(c=cache(batch=1), kd=one, vd=one, write=False)[0] == UNSUPPORTED
+
+
 def test_workspace_is_checked_and_only_needed_for_long_caches():
     lib, n = A._lib(), C.c_uint64()
     c, q = cache(max_pages=512, table_stride=512), tokens(tokens=1)

@@ -501,6 +501,34 @@ def test_cache_object_grows_trims_and_refuses():
     assert (c.attend(q)[0] == 0).all()
 
 
+def test_a_refused_append_leaves_the_cache_as_it_was():
+    c = A.KvCache(2, 2, 64, 128, page_tokens=32)
+    k = rand(1, 2, 40, 2, 64)
+    c.append(k[:, :5], k[:, :5])
+    was = [list(r) for r in c.table], list(c.free), list(c.lengths), c.pages.clone(), c.pool.clone()
+    for bad in (lambda: c.append(k.half(), k.half()), lambda: c.append(k, k[:, :39]), lambda: c.append(k[:1], k[:1]),
+                lambda: c.append(k[:, :, :1], k[:, :, :1]), lambda: c.append(k, k, [40]), lambda: c.append(k, k, [1, 1, 1]),
+                lambda: c.append(k, k, [-1, 1]), lambda: c.append(k[0], k[0])):
+        with pytest.raises(F.FluidError):
+            bad()
+        assert (c.table, c.free, c.lengths) == was[:3] and torch.equal(c.pages, was[3]) and torch.equal(c.pool, was[4])
+        assert c.kv_len.tolist() == c.lengths
+    c.append(k, k)
+    assert c.lengths == [45, 45]
+
+
+def test_trim_without_a_window_gives_nothing_back():
+    c = A.KvCache(1, 2, 64, 128, page_tokens=32)
+    k = rand(1, 1, 100, 2, 64)
+    c.append(k, k)
+    q = rand(2, 1, 1, 2, 64)
+    before = c.attend(q)
+    c.trim(0)
+    assert torch.equal(c.attend(q), before) and not c.free
+    with pytest.raises(F.FluidError, match="negative"):
+        c.trim(-1)
+
+
 def test_checks_hold_behind_a_call_of_the_same_shapes():
     block = A.pool_block(32, 64)
     pages, at, one = ints([0]).view(1, 1), ints([0]), ints([1])
