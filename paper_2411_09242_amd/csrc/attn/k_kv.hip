@@ -44,8 +44,8 @@ struct Run {
   int slot;              // the run's place in its page
   uint8_t* block;        // of the (page, head)
 
-  // false: none of the call's tokens has a place here
-  __device__ __forceinline__ bool find(const KvIoParams& p, int64_t item, int span) {
+  // false: none of the call's tokens is here
+  __device__ __forceinline__ bool locate(const KvIoParams& p, int64_t item, int span) {
     if (item >= p.items) return false;
     int x = (int)fdiv((uint32_t)item, p.div_heads);
     h = (int)item - x * p.c.kv_heads;
@@ -54,12 +54,15 @@ struct Run {
     start = uniform_load(p.start, b);
     n = clamp_len(p.count, b, p.tokens);
     first = (start & -(int64_t)span) + span * (int64_t)o;  // floor, negative starts too
-    if (n == 0 || first < 0 || first >= p.c.capacity || first >= start + n) return false;
+    return n != 0 && first >= 0 && first < p.c.capacity && first < start + n;
+  }
+  // false: the page holds no tokens; block is then page 0's
+  __device__ __forceinline__ bool place(const KvIoParams& p) {
     const int page = uniform_load(p.c.pages, b * p.c.table_stride + (first >> p.c.log_page));
-    if ((uint32_t)page >= (uint32_t)p.c.n_pages) return false;
+    const bool held = (uint32_t)page < (uint32_t)p.c.n_pages;
     slot = (int)first & ((1 << p.c.log_page) - 1);
-    block = p.c.pool + ((int64_t)page * p.c.kv_heads + h) * p.c.block;
-    return true;
+    block = p.c.pool + ((int64_t)(held ? page : 0) * p.c.kv_heads + h) * p.c.block;
+    return held;
   }
   // row of the call's tensors that holds token t of the run, if it is one
   __device__ __forceinline__ bool row(int t, int64_t& r) const {
@@ -89,15 +92,12 @@ template <typename T, int D>
 __global__ __launch_bounds__(256) void kv_write_kernel(KvIoParams p) {
   constexpr int G = D / 32;
   Run run;
-  if (!run.find(p, wave_index(), 8)) return;
+  if (!run.locate(p, wave_index(), 8)) return;
   const int lane = threadIdx.x & 31, half = (threadIdx.x >> 5) & 1, q = lane & 3, L = lane >> 2, t = nibble_element(L);
   int64_t row;
-  const bool mine = run.row(t, row);
-  // lane 4 L + q votes on the token that nibble L holds: a half's 32 votes
-  // are the mask of the nibbles of V to change
-  const uint32_t mask = (uint32_t)__ballot(mine);
-  const int P = 1 << p.c.log_page, slot = run.slot + t;
-  uint32_t* const base = (uint32_t*)run.block;
+  const bool within = run.row(t, row);
+  // the values are on their way while the page is looked up, and the words of
+  // V that keep some of their nibbles while the values are
   // parts 0 .. G - 1 are the groups of K, G .. 2 G - 1 those of V, two at a
   // time; lanes without a token of the call read one that is
   const int64_t from = min(max(row, (int64_t)0), (int64_t)run.n - 1);
@@ -108,6 +108,19 @@ __global__ __launch_bounds__(256) void kv_write_kernel(KvIoParams p) {
   for (int i = 0; i < G; ++i) {
     const T* const at = G == 1 ? (half ? vt : kt) : 2 * i < G ? kt + 32 * (2 * i + half) : vt + 32 * (2 * i - G + half);
     raw[i].load(at, 2 * i < G && !(G == 1 && half) ? p.k.vec : p.v.vec);
+  }
+  const bool mine = run.place(p) && within;
+  // lane 4 L + q votes on the token that nibble L holds: a half's 32 votes
+  // are the mask of the nibbles of V to change
+  const uint32_t mask = (uint32_t)__ballot(mine);
+  const int P = 1 << p.c.log_page, slot = run.slot + t;
+  uint32_t* const base = (uint32_t*)run.block;
+  uint32_t* const words = base + P * (D / 8 + G) + (slot >> 3) * D + 8 * q + t;  // of V, channel 8 q + t of a group
+  uint32_t old[G] = {};
+  if (mask != 0xffffffffu) {
+#pragma unroll
+    for (int i = 0; i < G; ++i)
+      if (2 * i + half >= G) old[i] = words[32 * ((2 * i + half) % G)];
   }
 #pragma unroll
   for (int i = 0; i < G; ++i) {
@@ -161,8 +174,7 @@ __global__ __launch_bounds__(256) void kv_write_kernel(KvIoParams p) {
       }
     } else {
       w = transpose_nibbles(w, L);  // now of channel 8 q + t
-      uint32_t* const to = base + P * (D / 8 + G) + (slot >> 3) * D + 32 * g + 8 * q + t;
-      *to = mask == 0xffffffffu ? w : (*to & ~mask) | (w & mask);
+      if (mask != 0) words[32 * g] = (old[i] & ~mask) | (w & mask);
       if (mine && q == 0) {
         uint16_t* const pair = (uint16_t*)(base + P * (D / 4 + G)) + ((slot >> 3) * G + g) * 16 + t;
         pair[0] = (uint16_t)s16;
@@ -207,7 +219,7 @@ __global__ __launch_bounds__(256) void kv_read_kernel(KvIoParams p) {
   using Tile = KvTile<D>;
   constexpr int G = Tile::G, WPL = Tile::WPL, NC = Tile::NC;
   Run run;
-  if (!run.find(p, wave_index(), kKvTile)) return;
+  if (!run.locate(p, wave_index(), kKvTile) || !run.place(p)) return;
   const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4, P = 1 << p.c.log_page;
   const Magic mg;
   Tile tile;
