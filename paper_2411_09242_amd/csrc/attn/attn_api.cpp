@@ -19,11 +19,10 @@ constexpr int64_t kMostGroups = (int64_t(1) << 31) - 1;
 void check_head_dim(int d) { require(d == 32 || d == 64 || d == 128, "head_dim must be 32, 64 or 128"); }
 
 TokensArg tokens_arg(const fluid_tokens* d, const void* p, const char* name) {
-  require(d != nullptr, std::string(name) + ": NULL description");
-  const std::string at = std::string(name) + ": ";
-  require(d->dtype == FLUID_F32 || d->dtype == FLUID_BF16, at + "dtype must be f32 or bf16");
-  require(d->batch >= 1 && d->tokens >= 1 && d->heads >= 1, at + "batch, tokens and heads must be at least 1");
-  require(d->tokens <= kMostTokens, at + "more than 2^30 tokens");
+  require(d != nullptr, name, ": NULL description");
+  require(d->dtype == FLUID_F32 || d->dtype == FLUID_BF16, name, ": dtype must be f32 or bf16");
+  require(d->batch >= 1 && d->tokens >= 1 && d->heads >= 1, name, ": batch, tokens and heads must be at least 1");
+  require(d->tokens <= kMostTokens, name, ": more than 2^30 tokens");
   check_head_dim(d->head_dim);
   const int32_t extent[3] = {d->batch, d->tokens, d->heads};
   const int el = dtype_bytes(d->dtype);
@@ -31,16 +30,16 @@ TokensArg tokens_arg(const fluid_tokens* d, const void* p, const char* name) {
   int64_t* const to[3] = {&a.sb, &a.st, &a.sh};
   for (int i = 0; i < 3; ++i) {
     if (extent[i] == 1) continue;  // its stride is never used
-    require(d->stride[i] >= 0 && d->stride[i] <= (int64_t(1) << 40), at + "strides must lie in 0 .. 2^40");
+    require(d->stride[i] >= 0 && d->stride[i] <= (int64_t(1) << 40), name, ": strides must lie in 0 .. 2^40");
     *to[i] = d->stride[i];
     if (d->stride[i] * el % 16) a.vec = 0;
   }
   if ((uintptr_t)p % 16) a.vec = 0;
-  require((uintptr_t)p % el == 0, at + "misaligned for its type");
+  require((uintptr_t)p % el == 0, name, ": misaligned for its type");
   return a;
 }
 TokensArg tokens_data(const fluid_tokens* d, const void* p, const char* name) {
-  require(p != nullptr, std::string(name) + ": NULL data");
+  require(p != nullptr, name, ": NULL data");
   return tokens_arg(d, p, name);
 }
 
@@ -50,7 +49,7 @@ void check_apart(const fluid_tokens* d, const char* name) {
   const int32_t extent[3] = {d->batch, d->tokens, d->heads};
   for (int i = 0; i < 3; ++i)
     require(extent[i] == 1 || d->stride[i] >= d->head_dim,
-            std::string(name) + ": an output's strides must be at least head_dim");
+            name, ": an output's strides must be at least head_dim");
 }
 
 int64_t block_bytes(const fluid_kv_cache* c) { return int64_t(5) * c->head_dim * c->page_tokens / 4; }

@@ -32,6 +32,13 @@ struct Error : std::runtime_error {
 inline void require(bool ok, const std::string& msg) {
   if (!ok) fail(FLUID_E_INVALID, msg);
 }
+// without building the message of a check that holds
+inline void require(bool ok, const char* msg) {
+  if (!ok) fail(FLUID_E_INVALID, msg);
+}
+inline void require(bool ok, const char* name, const char* msg) {
+  if (!ok) fail(FLUID_E_INVALID, std::string(name) + msg);
+}
 
 void set_last_error(const std::string& msg);
 
