@@ -125,6 +125,17 @@ __device__ __forceinline__ void store8<uint16_t>(uint16_t* p, bool vec, const fl
   }
 }
 
+// over a wavefront, the same for all lanes
+__device__ __forceinline__ int wave_total(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);  // from the lane 1, 2, 4, 8 before it in its row of 16
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);  // a row's last lane to the next row
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);  // lane 31 to the upper rows
+  return __builtin_amdgcn_readlane(v, 63);
+}
+
 // A value that all lanes read, by a scalar load: the lengths and page tables
 // are not written while a kernel runs.
 __device__ __forceinline__ int uniform_load(const int32_t* p, int64_t i) {
@@ -225,11 +236,55 @@ struct Share {
     first = split * per;
     end = min(first + per, item.range.count);
   }
+  // The k-th longest row tile of the heads head0, head0 + rank_step, .., by the
+  // position it starts at in units of a tile's rows, one share each; lane i
+  // counts those of the i-th head.  Workgroups go to the rank_units compute
+  // units in turn, so where each gets two at most the second ones come from the
+  // shortest on, and a unit with a long one has a short one beside it.
+  __device__ __forceinline__ bool by_length(const AttnParams& p, int head0, int k) {
+    const int lane = threadIdx.x & 63, log_tile = __builtin_ctz(p.row_tile);
+    int n = p.kv_tokens, queries = p.q_tokens, tiles = 0, low = 0;
+    if (lane < p.rank_heads) {
+      const int b = (int)fdiv(head0 + p.rank_step * lane, p.div_heads);
+      if (p.kv_len) n = min(max(p.kv_len[b], 0), n);
+      if (p.q_len) queries = min(max(p.q_len[b], 0), queries);
+      tiles = (queries * p.group + p.row_tile - 1) >> log_tile;
+      low = (int)min(((int64_t)max(n - queries, 0) * p.group) >> log_tile, (int64_t)kMostLevels);
+    }
+    // how many start at x or later
+    auto from = [&](int x) { return wave_total(min(max(low + tiles - x, 0), tiles)); };
+    const int all = from(0);
+    if (k >= all) return false;
+    if (all <= 2 * p.rank_units && k >= p.rank_units) k = all - 1 - (k - p.rank_units);
+    int x = 0, end = p.levels - 1;
+    while (x < end) {
+      const int mid = (x + end) >> 1;
+      if (from(mid + 1) <= k) end = mid;
+      else x = mid + 1;
+    }
+    k -= from(x + 1);
+    const bool has = low <= x && x < low + tiles;
+    const int before = __popcll(__ballot(has) & ((uint64_t(1) << lane) - 1));
+    const int i = __builtin_ctzll(__ballot(has && before == k)), head = head0 + p.rank_step * i;
+    item.b = (int)fdiv(head, p.div_heads);
+    item.h = head - item.b * p.kv_heads;
+    item.n = __builtin_amdgcn_readlane(n, i);
+    const int ql = __builtin_amdgcn_readlane(queries, i), rt = x - __builtin_amdgcn_readlane(low, i);
+    item.rows = ql * p.group;
+    item.p0 = item.n - ql;
+    index = head * p.row_tiles + (p.row_tiles - 1 - rt);
+    split = 0;
+    item.tile(p, rt);
+    steps(p);
+    return true;
+  }
   // false: nothing to do
   __device__ __forceinline__ bool find(const AttnParams& p, int block) {
     // Workgroups go to the eight XCDs, which have an L2 each, in turn.  Heads
-    // are dealt to them likewise, so that a head's keys are read into one L2
-    // and the sequences of a ragged batch are spread over all.
+    // are dealt to them likewise where that comes out even, so that a head's
+    // keys are read into one L2 and the sequences of a ragged batch are spread
+    // over all.
+    if (p.rank_heads) return p.by_xcd ? by_length(p, block & 7, block >> 3) : by_length(p, 0, block);
     if (p.by_xcd) {
       const int j = block >> 3, head = (int)fdiv(j, p.div_head), of = p.row_tiles * p.splits;
       block = ((block & 7) + 8 * head) * of + (j - head * of);

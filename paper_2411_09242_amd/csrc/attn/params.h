@@ -52,12 +52,18 @@ struct AttnParams {
   int32_t chunk;   // steps of a share
   FastDiv div_group, div_tiles, div_heads, div_splits;
   int32_t by_xcd;     // 1: a kv head's workgroups on one XCD
+  int32_t rank_heads;  // > 0: row tiles from the longest on, of so many heads together
+  int32_t rank_step, rank_units;  // from one of the heads to the next; compute units they have
+  int32_t levels;      // past the last place that a row tile can start at
   FastDiv div_head;   // by a kv head's workgroups
   float* ws;       // splits > 1: [item][split] of row_tile maxima, sums and rows of partial sums
 };
 
 // tokens of a step over the 4-bit cache, and over bf16 and fp32 keys and values
 constexpr int kKvTile = 32, kBf16Tile = 64, kF32Tile = 32;
+
+// Bound on the places, in row tiles, by which long rows are told from short ones.
+constexpr int kMostLevels = 1 << 24;
 
 // Wavefronts of a workgroup that has an item's tokens to itself: as many as the
 // registers of a compute unit hold.

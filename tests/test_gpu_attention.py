@@ -261,6 +261,32 @@ def test_attention(dtype, D, T, N, q_len, kv_len, H, Hk, causal, window, sinks):
     check(out, q, k, v, ql, kl, D ** -0.5, causal, window, sinks, dtype, False, left=4.0)
 
 
+MANY = [  # batch, T, N, heads, kv_heads, window, sinks, ragged: hundreds of row tiles, taken in an order of their own
+    (1, 700, 700, 48, 48, 0, 0, False),     # up to 64 of them to an XCD
+    (4, 600, 650, 16, 16, 0, 0, True),
+    (16, 260, 300, 16, 16, 50, 3, True),    # more
+    (3, 520, 1030, 32, 8, 0, 0, True),      # shared keys, queries behind them
+    (1, 2900, 2900, 12, 12, 100, 2, False),  # heads that do not come out even over the XCDs, up to 512 tiles
+    (3, 700, 800, 100, 20, 0, 0, True),     # and more
+    (64, 20, 40, 16, 16, 0, 0, True),       # more heads to an XCD than lanes
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B, T, N, H, Hk, window, sinks, ragged", MANY)
+def test_attention_of_many_rows(dtype, B, T, N, H, Hk, window, sinks, ragged):
+    D = 32
+    q, k, v = rand(1, B, T, H, D, dtype=dtype), rand(2, B, N, Hk, D, dtype=dtype), rand(3, B, N, Hk, D, dtype=dtype)
+    ql, kl = [T] * B, [N] * B
+    if ragged:
+        ql = [T * (b * 7 % 5) // 4 for b in range(B)]
+        kl = [N - N * (b * 3 % 4) // 4 for b in range(B)]
+    out = torch.full_like(q, 4.0)
+    A.attention(q, k, v, q_len=ints(ql) if ragged else None, kv_len=ints(kl) if ragged else None, window=window,
+                sinks=sinks, out=out)
+    check(out, q, k, v, ql, kl, D ** -0.5, True, window, sinks, dtype, False, left=4.0)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("how", ["heads_first", "padded", "odd"])
 @pytest.mark.parametrize("D", [32, 128])
