@@ -67,6 +67,19 @@ class Decoder:
         self.caches = [A.KvCache(batch, kv_heads, head_dim, max_tokens, page_tokens=page_tokens) for _ in range(layers)]
         self.runs = {}
 
+    plans = {}  # of all decoders, by graph
+
+    def _plan(self, desc):
+        """Graph, layouts and arena.  A plan follows measured times: another
+        measurement may choose other kernels, which round elsewhere, so a graph
+        is measured once and decoders of the same shapes give the same bits."""
+        F, key = self.F, repr(desc)
+        if key not in self.plans:
+            graph = F.Graph.from_desc(desc)
+            plan = F.LayoutPlan(graph, F.CostTable.measure(graph))
+            self.plans[key] = graph, plan, F.ArenaPlan(graph, plan)
+        return self.plans[key]
+
     def _runs(self, T):
         """Executors of both graphs for every layer, for T tokens a sequence."""
         if T not in self.runs:
@@ -74,10 +87,7 @@ class Decoder:
             q, kv = self.H * self.D, self.Hk * self.D
 
             def make(desc, consts):
-                graph = F.Graph.from_desc(desc)
-                table = F.CostTable.measure(graph)
-                plan = F.LayoutPlan(graph, table)
-                arena = F.ArenaPlan(graph, plan)
+                graph, plan, arena = self._plan(desc)
                 return [F.Executor(graph, plan, arena, c, [torch.zeros(s) for s in desc["inputs"]]) for c in consts]
             self.runs[T] = list(zip(
                 make(project_desc(self.B, T, self.C, q, kv), [a for a, _ in self.weights]),
