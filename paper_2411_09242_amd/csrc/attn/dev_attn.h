@@ -236,9 +236,10 @@ struct Share {
     first = split * per;
     end = min(first + per, item.range.count);
   }
-  // The k-th longest row tile of the heads head0, head0 + rank_step, .., by the
-  // position it starts at in units of a tile's rows, one share each; lane i
-  // counts those of the i-th head.  Workgroups go to the rank_units compute
+  // The k-th longest row tile of the heads head0, head0 + rank_step, .., one
+  // share each: by the position it starts at in units of a tile's rows, or by
+  // the sequence's length where no mask cuts it off.  Lane i counts those of the
+  // i-th head.  Workgroups go to the rank_units compute
   // units in turn, so where each gets two at most the second ones come from the
   // shortest on, and a unit with a long one has a short one beside it.
   __device__ __forceinline__ bool by_length(const AttnParams& p, int head0, int k) {
@@ -249,7 +250,9 @@ struct Share {
       if (p.kv_len) n = min(max(p.kv_len[b], 0), n);
       if (p.q_len) queries = min(max(p.q_len[b], 0), queries);
       tiles = (queries * p.group + p.row_tile - 1) >> log_tile;
-      low = (int)min(((int64_t)max(n - queries, 0) * p.group) >> log_tile, (int64_t)kMostLevels);
+      const int64_t at = p.causal ? ((int64_t)max(n - queries, 0) * p.group) >> log_tile
+                                  : (int64_t)(n >> log_tile) * p.row_tiles;
+      low = (int)min(at, (int64_t)kMostLevels);
     }
     // how many start at x or later
     auto from = [&](int x) { return wave_total(min(max(low + tiles - x, 0), tiles)); };

@@ -288,6 +288,19 @@ def test_attention_of_many_rows(dtype, B, T, N, H, Hk, window, sinks, ragged):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B, T, N, H, Hk, window", [(4, 600, 650, 16, 16, 0), (7, 500, 500, 12, 12, 40), (5, 300, 900, 32, 8, 0)])
+def test_attention_of_many_rows_in_both_directions(dtype, B, T, N, H, Hk, window):
+    D = 32
+    q, k, v = rand(1, B, T, H, D, dtype=dtype), rand(2, B, N, Hk, D, dtype=dtype), rand(3, B, N, Hk, D, dtype=dtype)
+    ql = [T * (b * 7 % 5) // 4 for b in range(B)]
+    kl = [N - N * (b * 3 % 4) // 4 for b in range(B)]
+    kl[-1] = 0
+    out = torch.full_like(q, 4.0)
+    A.attention(q, k, v, q_len=ints(ql), kv_len=ints(kl), causal=False, window=window, sinks=2, out=out)
+    check(out, q, k, v, ql, kl, D ** -0.5, False, window, 2, dtype, False, left=4.0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("how", ["heads_first", "padded", "odd"])
 @pytest.mark.parametrize("D", [32, 128])
 def test_attention_strides(dtype, how, D):
