@@ -211,14 +211,18 @@ AttnParams plan_attention(const fluid_attention_opts* opts, const fluid_tokens* 
   // One round of workgroups, one to a compute unit.  512 queries of 32 heads
   // behind 7680 tokens, bf16: 121 us in 128 workgroups, 80 in 256 or 512, 91 in
   // 1024; 64 queries behind 4032: 64 us in 16, 19 in 256, 23 in 512; fp32: 437,
-  // 48 and 60.  A short bf16 loop is not worth a second launch: 512 queries of
-  // 12 heads over 512 tokens 11.2 us in one, 13.3 in two (fp32: 28.5 and 18.3).
-  const bool brief = qd->dtype == FLUID_BF16 && visible <= 512;
+  // 48 and 60.  A short loop is not worth a second launch: bf16, 512 queries of
+  // 12 heads over 512 tokens 11.2 us in one, 13.3 in two; fp32, 4 x 130 tokens
+  // of 8 heads 13.0 and 15.4 (4 x 180: 14.2 and 13.9; 512 of 12 heads 28.5 and 18.3).
+  const bool bf16 = qd->dtype == FLUID_BF16, brief = visible <= (bf16 ? 512 : 160);
   plan_shares(p, visible, brief ? 1 : 256, 2);
-  // Two teams where that still is one round of workgroups.  fp32 with 128
-  // channels has no room for a second team's stages.
+  // Two teams where that still is one round of workgroups, but not to join a
+  // single step, or two short ones, of 32 tokens: 16 bf16 tokens of 8 heads 6.5 us
+  // with one team, 7.8 with two; 100 tokens (two steps) 7.8 and 7.3; fp32, a
+  // query each over 50 tokens 8.1 and 8.5.  fp32 with 128 channels has no room
+  // for a second team's stages.
   const int64_t heads = int64_t(p.batch) * p.kv_heads, groups = heads * p.row_tiles * p.splits;
-  p.teams = groups <= 256 && !(qd->dtype == FLUID_F32 && qd->head_dim == 128) ? 2 : 1;
+  p.teams = groups <= 256 && p.chunk > (bf16 ? 1 : 2) && (bf16 || qd->head_dim < 128) ? 2 : 1;
   p.by_xcd = heads % 8 == 0;
   // More than one workgroup to a compute unit: the longest rows first, whatever
   // their head, where a wavefront's lanes can hold an XCD's heads, or all of
@@ -228,8 +232,8 @@ AttnParams plan_attention(const fluid_attention_opts* opts, const fluid_tokens* 
   // up to 700 tokens 50.7 and 55.2, of up to 500 in both directions 20.5 and 28.7.
   p.rank_step = p.by_xcd ? 8 : 1;
   p.rank_units = p.by_xcd ? 32 : 256;
-  p.levels = (int32_t)std::min<int64_t>(int64_t(p.kv_tokens) * (p.causal ? p.group : p.row_tiles) / p.row_tile, kMostLevels) +
-             p.row_tiles + 1;
+  const int64_t places = int64_t(p.kv_tokens) * (p.causal ? p.group : p.row_tiles) / p.row_tile;
+  p.levels = (int32_t)std::min<int64_t>(places, kMostLevels) + p.row_tiles + 1;
   if (p.splits == 1 && groups > 256 && heads / p.rank_step <= 64) p.rank_heads = (int32_t)(heads / p.rank_step);
   p.div_head = make_fastdiv(p.row_tiles * p.splits);
   return p;

@@ -3,14 +3,14 @@
 // LDS without registers, one tile of 64 tokens ahead of the products; V is
 // read back by transposing reads.
 //
-// 8192 queries of 32 heads of 128 (8 of keys), window 2048: 270 us (300 on a
-// slower card), 890 TFLOP/s of the products needed, where a library product of
-// 8192^3 reaches 1140.  MFMA are 47 % and vector instructions 44 % of the
-// cycles, at a clock of 1.8 GHz of 2.4: power bounds it.  The products alone,
-// without copies and weights, take 193 us; with LDS operands read further
-// ahead, copies a step and a half ahead behind two barriers, or one of a
-// SIMD's two wavefronts preferred the time is the same or worse.  2048 queries
-// (window 1024) take 48 us, most of it the 18 steps of the longest rows.
+// 8192 queries of 32 heads of 128 (8 of keys), window 2048: 267 to 292 us (by
+// card), 820 to 900 TFLOP/s of the products needed, where a library product of 8192^3
+// reaches 1140.  MFMA are 47 % and vector instructions 44 % of the cycles, at a
+// clock of 1.8 GHz of 2.4: power bounds it.  The products alone, without copies
+// and weights, take 193 us; with LDS operands read further ahead, copies a step
+// and a half ahead behind two barriers, or one of a SIMD's two wavefronts
+// preferred the time is the same or worse.  2048 queries of 32 heads (window
+// 1024) take 42 to 48 us: two workgroups to a compute unit, of 2 to 19 steps each.
 #include "attn_rows.h"
 #include "launch_attn.h"
 
@@ -27,11 +27,13 @@ __device__ __forceinline__ void copy_to_lds(const void* from, void* to) {
 }
 
 // One team of narrow heads fits a SIMD three times: 8 x 2048 causal queries of
-// 16 heads of 64 channels take 126 us, 16 x 1024 of 32 channels 64, with two of them 143 and 72.
+// 16 heads of 64 channels take 126 us, 16 x 1024 of 32 channels 64; with two of
+// them 143 and 72.
 constexpr int waves_per_simd(int D, int teams) { return teams == 1 && D < 128 ? 3 : 2; }
 
 template <int D, int TEAMS, bool VEC>
-__global__ __launch_bounds__(kTeam * TEAMS) __attribute__((amdgpu_waves_per_eu(waves_per_simd(D, TEAMS), waves_per_simd(D, TEAMS))))
+__global__ __launch_bounds__(kTeam * TEAMS)
+__attribute__((amdgpu_waves_per_eu(waves_per_simd(D, TEAMS), waves_per_simd(D, TEAMS))))
 void attention_bf16_kernel(AttnParams p) {
   using At = Bf16Place<D>;
   constexpr int PPR = D / 8, PIECES = BN * PPR, CT = D / 32;

@@ -10,7 +10,6 @@ namespace fluid {
 
 namespace {
 
-
 // Row `row` of kv head x: its first share, and its place in it.
 struct JoinRow {
   Share sh;

@@ -15,8 +15,9 @@
 // queries over 8192 tokens and 32 heads, with the read: 161 us, 189 with them).
 // Writing has 25 vector instructions a value, 10 us of the 18.6 that 2048
 // tokens (44 MB) take; all wavefronts of so many fit the GPU at once, so loads
-// and arithmetic overlap little.  One token or 16 take 5 to 7 us, a chain of
-// three dependent loads (lengths, page, values) and the launch.
+// and arithmetic overlap little.  One token or 16 take 5 to 6 us: the
+// launch and a chain of dependent loads (lengths; the page, beside the values to
+// write; the words to read, or those that keep some of their nibbles).
 #include "kv_tile.h"
 #include "launch_attn.h"
 
