@@ -79,7 +79,8 @@ void attention_bf16_kernel(AttnParams p) {
       }
     }
   };
-  // Values that are no numbers become zeros (Rows::add_odd).
+  // Values that are no numbers become zeros, in the tiles that Rows::add_odd
+  // goes through.
   uint32_t dirty = 0;
   auto clean = [&](uint16_t* sv) {
 #pragma nounroll
@@ -102,8 +103,8 @@ void attention_bf16_kernel(AttnParams p) {
     bool masked = false;  // some team's tile is
 #pragma unroll
     for (int i = 0; i < TEAMS; ++i) masked |= at + i < w.u1 && !w.whole_for_all(w.start(at + i));
-    if (masked) {
-      if (u < w.u1) clean(sv);
+    if (masked) {  // a tile that all rows see whole may have one beside it that they do not
+      if (u < w.u1 && !w.whole_for_all(t0)) clean(sv);
       __syncthreads();
     }
     if (u + TEAMS < w.u1) stage(u + TEAMS, next_k, next_v);

@@ -332,6 +332,36 @@ def test_what_a_row_does_not_see_may_be_anything(dtype, value, causal, window, s
                 assert np.array_equal(got[0, i], clean[0, i]), (at, i)
 
 
+PAIRED = [  # T, N, heads, kv_heads, causal, window, sinks: tiles that all rows see whole beside tiles that they do not
+    (1, 100, 2, 2, True, 0, 0),       # the last tile is cut off by the length
+    (1, 192, 2, 2, True, 100, 0),     # the first by the window
+    (1, 300, 4, 1, True, 170, 70),    # the sinks' second tile too
+    (64, 384, 4, 1, True, 0, 0),      # the diagonal, behind cached keys
+    (70, 333, 4, 1, True, 77, 5),
+    (5, 250, 2, 1, False, 101, 0),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("T, N, H, Hk, causal, window, sinks", PAIRED)
+def test_what_a_row_sees_is_never_dropped(dtype, value, T, N, H, Hk, causal, window, sinks):
+    D = 64
+    q, k, v = rand(0, 1, T, H, D, dtype=dtype), rand(1, 1, N, Hk, D, dtype=dtype), rand(2, 1, N, Hk, D, dtype=dtype)
+    clean = host(A.attention(q, k, v, causal=causal, window=window, sinks=sinks))
+    for at in sorted({*range(5, N, 32), N - 1}):
+        v2 = v.clone()
+        v2[0, at, 0, 7] = value
+        got = host(A.attention(q, k, v2, causal=causal, window=window, sinks=sinks))
+        for i in range(T):
+            for h in range(H // Hk):
+                if OA.sees(N - T + i, at, N, causal, window, sinks):
+                    assert not np.isfinite(got[0, i, h, 7]), (at, i, h)
+                    assert np.isfinite(np.delete(got[0, i, h], 7)).all()
+                else:
+                    assert np.array_equal(got[0, i, h], clean[0, i, h]), (at, i, h)
+
+
 def test_large_and_small_scores():
     for dtype in ("bf16", "f32"):
         q, k, v = (rand(i, 1, 90, 2, 64, dtype=dtype) for i in range(3))
