@@ -47,7 +47,10 @@ typedef struct {
  *     n = s > 0 ? clamp(rint((c - b) / s) - 16, 0, 15) : 0
  * in fp32, ties to even.  A group that holds an infinity or a NaN reads back
  * as NaN in all its 32 channels.  Groups whose values are all below 2^-14
- * lose precision with the float16 pair.
+ * lose precision with the float16 pair.  Values of pairs made so are within
+ * float16; attention may take a group whose values at nibbles 0 and 15 are not
+ * for NaN.  The pool need not be cleared: no call uses what was not written,
+ * but for tokens that a length says are there.
  *
  * pool: [n_pages][kv_heads][block], block = 5 * head_dim * page_tokens / 4
  * bytes, 16-byte aligned.  A block holds page_tokens P of one kv head, with

@@ -52,8 +52,17 @@ __device__ __forceinline__ float col_sum(float v) {
   return v + __shfl_xor(v, 32);
 }
 
-// Whether the low f16 of w is an infinity or a NaN.
-__device__ __forceinline__ uint32_t odd_half(uint32_t w) { return (w & 0x7c00u) == 0x7c00u; }
+// Which halves of a word of pairs (two tokens' s and b) may stand for an infinity
+// or a NaN, as bits 0 and 1: values lie between those of nibbles 0 and 15.  Slots
+// that were never written hold any bytes, and their finite pairs may have values
+// past f16's range.
+__device__ __forceinline__ uint32_t odd_pairs(uint32_t s, uint32_t b) {
+  const f16x2 ss = __builtin_bit_cast(f16x2, s), bb = __builtin_bit_cast(f16x2, b);
+  const uint32_t lo = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(f16x2{16, 16}, ss, bb));
+  const uint32_t hi = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(f16x2{31, 31}, ss, bb));
+  auto none = [](uint32_t w, uint32_t exponent) -> uint32_t { return (w & exponent) == exponent; };
+  return none(lo, 0x7c00u) | none(hi, 0x7c00u) | (none(lo, 0x7c000000u) | none(hi, 0x7c000000u)) << 1;
+}
 
 template <typename T, int D, int MT, int NW>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(NW == 16 ? 4 : MT == 1 && NW == 4 ? 3 : 2)))
@@ -185,16 +194,13 @@ void kv_attention_kernel(AttnParams p) {
           for (int r = 0; r < 4; ++r)
             if (dark | !eye[mt].sees(t0 + 8 * g4 + 4 * i + r)) sc[mt][i][r] = -INFINITY;
       // Weight 0 times a value that is no number would still be none.  So the
-      // groups that are none become zeros here, and NaN goes into the sums of
+      // groups that may hold one become zeros here, and NaN goes into the sums of
       // the rows that do see them.
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
         uint32_t odd = 0;  // of this lane's octet and group
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          odd |= (odd_half(tile.vs[c][i]) | odd_half(tile.vb[c][i])) << (2 * i);
-          odd |= (odd_half(tile.vs[c][i] >> 16) | odd_half(tile.vb[c][i] >> 16)) << (2 * i + 1);
-        }
+        for (int i = 0; i < 4; ++i) odd |= odd_pairs(tile.vs[c][i], tile.vb[c][i]) << (2 * i);
         if (__builtin_expect(__ballot(odd != 0) != 0, 0)) {
           // a lane's sums belong to the channels 64 c + 16 g4 .. +15, of the
           // group that the source lanes 8 (g4 / 2) of each sixteen hold

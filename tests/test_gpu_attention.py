@@ -476,6 +476,35 @@ def test_kv_attention_unseen_tokens_may_be_odd_and_pages_gone(dtype, window, sin
         assert np.array_equal(host(A.kv_attention(pg.pool, pg.pages, q, ints([n]), window=window, sinks=sinks)), clean)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [32, 64, 128])
+@pytest.mark.parametrize("fill", [0x70, 0x7B, 0xFB, 0xFF])
+def test_kv_attention_over_a_pool_that_was_never_cleared(dtype, D, fill):
+    """Pairs of any bytes: 0x70 and 0x7B are finite, their values past float16."""
+    H, P, lens = 2, 64, [101, 1, 37]
+    k, v = rand(2, 3, 101, H, D, dtype=dtype), rand(3, 3, 101, H, D, dtype=dtype)
+    pools = [Paged(lens, H, D, P, fill=f) for f in (0, fill)]
+    for T, window, sinks in ((1, 0, 0), (5, 0, 0), (5, 20, 0), (20, 9, 2)):
+        q = rand(4, 3, T, 4, D, dtype=dtype)
+        got = []
+        for pg in pools:
+            A.kv_write(pg.pool, pg.pages, k, v, ints([0] * 3), ints(lens))
+            got.append(A.kv_attention(pg.pool, pg.pages, q, ints(lens), window=window, sinks=sinks))
+        assert got[0].isfinite().all() and torch.equal(*got)
+    # tokens that the window hides were never written, their page is in the table or is not, and page 0 is like that
+    for dark in (False, True):
+        got = []
+        for f in (0, fill):
+            pg = Paged([160], H, D, 32, fill=f, spare=1)
+            pg.pages.copy_(torch.tensor([[1, 2, 3, 4, 5]], dtype=torch.int32))
+            A.kv_write(pg.pool, pg.pages, k[:1, :53], v[:1, :53], ints([107]))
+            if dark:
+                pg.pages[0, :3] = -1
+            q = rand(4, 1, 9, 4, D, dtype=dtype)
+            got.append(A.kv_attention(pg.pool, pg.pages, q, ints([160]), window=40))
+        assert got[0].isfinite().all() and torch.equal(*got)
+
+
 def test_pool_and_strides_past_32_bits():
     D, P, H = 128, 64, 8
     n = (5 << 30) // (H * A.pool_block(P, D))
