@@ -74,6 +74,7 @@ struct Rows {
   Sight eye;
   const T *q, *k, *v;
   float m, l;
+  bool wide;  // some row of the wavefront is past_fused
   f32x16 acc[CT];
 
   __device__ __forceinline__ explicit Rows(const AttnParams& p_) : p(p_) {}
@@ -106,6 +107,7 @@ struct Rows {
     v = (const T*)p.v.p + it.b * p.v.sb + it.h * p.v.sh;
     m = kLow;
     l = 0.0f;
+    wide = false;
 #pragma unroll
     for (int c = 0; c < CT; ++c) acc[c] = f32x16{};
     return true;
@@ -138,18 +140,29 @@ struct Rows {
 #pragma unroll
       for (int e = 0; e < 16; ++e) top = fmaxf(top, s[i][e]);
     top *= p.cs;
-    if (__ballot(top > m + kRowSlack)) {
+    if (__ballot(top - m > kRowSlack)) {
       const float m1 = fmaxf(m, fmaxf(top, __shfl_xor(top, 32)));
       const float a = __builtin_amdgcn_exp2f(m - m1);
       m = m1;
       l *= a;
 #pragma unroll
       for (int c = 0; c < CT; ++c) acc[c] *= a;
+      wide = __ballot(past_fused(m)) != 0;
+    }
+    float factor = p.cs, shift = -m;
+    if (__builtin_expect(wide, 0)) {
+#pragma clang fp contract(off)
+#pragma unroll
+      for (int i = 0; i < NT; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[i][e] = s[i][e] * p.cs - m;
+      factor = 1.0f;
+      shift = 0.0f;
     }
 #pragma unroll
     for (int i = 0; i < NT; ++i)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) s[i][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i][e], p.cs, -m));
+      for (int e = 0; e < 16; ++e) s[i][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i][e], factor, shift));
   }
 
   // Weight 0 times a value that is no number would still be none, so such

@@ -13,6 +13,13 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr float kLow = -3.0e38f;  // a running maximum before the first score
 
+// A weight is 2 to the power of score * scale - maximum, fused: the product's
+// rounding, which the maximum has, is left out of it.  That is at most 1/8 up to
+// here, but 2^(m - 24) at 2^m: maxima from 2^31 on would make infinite weights, so
+// rows past this bound have their products rounded first.
+constexpr float kFusedMost = 4194304.0f;
+__device__ __forceinline__ bool past_fused(float m) { return (fabsf(m) > kFusedMost) & (m != kLow); }
+
 template <int CTRL>
 __device__ __forceinline__ float dpp(float v) {
   return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xf, 0xf, true));

@@ -149,11 +149,13 @@ void kv_attention_kernel(AttnParams p) {
   }
 
   float m[MT], l[MT];
+  bool wide[MT];  // some row is past_fused
   f32x4 acc[MT][NC][WPL];
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
     m[mt] = kLow;
     l[mt] = 0.0f;
+    wide[mt] = false;
 #pragma unroll
     for (int c = 0; c < NC; ++c)
 #pragma unroll
@@ -232,7 +234,7 @@ void kv_attention_kernel(AttnParams p) {
 #pragma unroll
       for (int e = 1; e < 8; ++e) top = fmaxf(top, sc[mt][e >> 2][e & 3]);
       top *= cs[mt];
-      if (__ballot(top > m[mt] + kSlack)) {
+      if (__ballot(top - m[mt] > kSlack)) {
         const float m1 = fmaxf(m[mt], col_max(top));
         const float a = __builtin_amdgcn_exp2f(m[mt] - m1);
         m[mt] = m1;
@@ -241,12 +243,20 @@ void kv_attention_kernel(AttnParams p) {
         for (int c = 0; c < NC; ++c)
 #pragma unroll
           for (int j = 0; j < WPL; ++j) acc[mt][c][j] *= a;
+        wide[mt] = __ballot(past_fused(m[mt])) != 0;
       }
-      const float shift = kPBits - m[mt];
+      float factor = cs[mt], shift = kPBits - m[mt];
+      if (__builtin_expect(wide[mt], 0)) {
+#pragma clang fp contract(off)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sc[mt][e >> 2][e & 3] = sc[mt][e >> 2][e & 3] * cs[mt] - m[mt];
+        factor = 1.0f;
+        shift = kPBits;
+      }
 #pragma unroll
       for (int e = 0; e < 8; e += 2) {
-        const f32x2 f = {__builtin_amdgcn_exp2f(__builtin_fmaf(sc[mt][e >> 2][e & 3], cs[mt], shift)),
-                         __builtin_amdgcn_exp2f(__builtin_fmaf(sc[mt][e >> 2][(e & 3) + 1], cs[mt], shift))};
+        const f32x2 f = {__builtin_amdgcn_exp2f(__builtin_fmaf(sc[mt][e >> 2][e & 3], factor, shift)),
+                         __builtin_amdgcn_exp2f(__builtin_fmaf(sc[mt][e >> 2][(e & 3) + 1], factor, shift))};
         l[mt] += f[0];
         l[mt] += f[1];
         const f16x2 hi = __builtin_convertvector(f, f16x2);

@@ -371,6 +371,52 @@ def test_large_and_small_scores():
         check(A.attention(*big), *big, [90], [90], 0.125, True, 0, 0, dtype, False)
 
 
+SCORES = [1e6, 1e10, 1e20, 1e36]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("size", SCORES + [-x for x in SCORES])
+def test_scores_of_any_size(dtype, size):
+    """Scores of `size` times 1 .. 100 / 64, far further apart than their
+    rounding: a row is the value of its highest alone (1e36: scores up to
+    1.6e36, sums within fp32)."""
+    D, N = 64, 100
+    q, k, v = torch.zeros(1, N, 1, D), torch.zeros(1, N, 1, D), rand(1, 1, N, 1, D, dtype=dtype)
+    q[..., 3] = np.sign(size) * 2.0 ** 60 if abs(size) > 1e19 else np.sign(size)
+    k[0, :, 0, 3] = (1 + torch.arange(N)) / 64 * (abs(size) / q[..., 3].abs().max())
+    q, k = q.to(DT[dtype]).cuda(), k.to(DT[dtype]).cuda()
+    for T in (1, 5, N):
+        got = A.attention(q[:, N - T:], k, v, scale=1.0)
+        want = v[:, N - T:] if size > 0 else v[:, :1].expand(1, T, 1, D)
+        # weights cancel but for a few fp32 roundings
+        assert ((got.float() - want.float()).abs() <= want.float().abs() * 2.0 ** -20).all(), T
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("size", SCORES + [-x for x in SCORES])
+@pytest.mark.parametrize("N", [100, 3000])
+def test_scores_of_any_size_over_the_cache(dtype, size, N):
+    D = 64
+    pg = Paged([N], 1, D, 64)
+    k, v = torch.zeros(1, N, 1, D, device="cuda"), rand(1, 1, N, 1, D, dtype=dtype)
+    k[0, :, 0, 3] = (1 + torch.arange(N, device="cuda") % 200) / 64
+    A.kv_write(pg.pool, pg.pages, k.to(DT[dtype]), v, ints([0]))
+    kk, vv = torch.zeros(1, N, 1, D, device="cuda"), torch.zeros(1, N, 1, D, device="cuda")
+    A.kv_read(pg.pool, pg.pages, ints([0]), kk, vv)
+    kk = host(kk)[0, :, 0, 3]
+    for T in (1, 5):
+        q = torch.zeros(1, T, 1, D, device="cuda")
+        q[..., 3] = size
+        got = host(A.kv_attention(pg.pool, pg.pages, q.to(DT[dtype]), ints([N]), scale=1.0))
+        for i in range(T):
+            x = kk[:N - T + 1 + i] * np.sign(size)
+            best = x == x.max()
+            # all products are exact but for q's rounding, the same for all: ties have one weight
+            want = host(vv)[0, :N - T + 1 + i, 0][best].mean(0)
+            tol = np.abs(host(vv)[0, :N - T + 1 + i, 0][best]).mean(0) * (2.0 ** -8 if dtype == "bf16" else 2.0 ** -19)
+            assert (np.abs(got[0, i, 0] - want) <= tol + 1e-30).all(), (T, i)
+
+
 CACHED = [  # T, heads, kv_heads, kv_len, q_len, window, sinks, page
     (1, 2, 2, [1, 0, 31], None, 0, 0, 32),
     (1, 8, 2, [33, 300, 64], None, 0, 0, 64),
