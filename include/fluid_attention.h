@@ -81,8 +81,10 @@ typedef struct {
  * j < kv_len with
  *     j <= p                              if causal
  *     |p - j| < window  or  j < sinks     if window > 0
- * A row that sees no token gets zeros.  A token that a row does not see
- * contributes nothing to it, whatever its key and value hold. */
+ * A row that sees no token gets zeros, and so does one whose scores are all
+ * minus infinity.  A token that a row does not see contributes nothing to it,
+ * whatever its key and value hold.  Scores times log2(e) are held in fp32: past
+ * 2.3e38 a score is infinite. */
 typedef struct {
   float scale; /* positive, finite */
   int32_t causal;

@@ -11,7 +11,9 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-constexpr float kLow = -3.0e38f;  // a running maximum before the first score
+// A running maximum before the first score: none is below it, so a row that sees
+// tokens gives weight to some.
+constexpr float kLow = -3.402823466e38f;
 
 // A weight is 2 to the power of score * scale - maximum, fused: the product's
 // rounding, which the maximum has, is left out of it.  That is at most 1/8 up to

@@ -417,6 +417,22 @@ def test_scores_of_any_size_over_the_cache(dtype, size, N):
             assert (np.abs(got[0, i, 0] - want) <= tol + 1e-30).all(), (T, i)
 
 
+def test_scores_down_to_the_lowest_are_seen():
+    """Rows whose scores are all the same, down to -2.3e38, are means of what
+    they see; those of minus infinity alone are zeros."""
+    D, N = 32, 40
+    for dtype in ("bf16", "f32"):
+        v = torch.ones(1, N, 1, D, dtype=DT[dtype], device="cuda")
+        for score in (1e37, -1e37, -2.2e38, -2.3e38):
+            q, k = torch.zeros(1, N, 1, D, device="cuda"), torch.zeros(1, N, 1, D, device="cuda")
+            q[..., 0], k[..., 0] = 1e19, score / 1e19
+            for T in (1, N):
+                got = A.attention(q[:, :T].to(DT[dtype]), k.to(DT[dtype]), v, scale=1.0)
+                assert ((got.float() - 1).abs() <= 2.0 ** -20).all(), (score, T)
+        k[..., 0] = -float("inf")
+        assert (A.attention(q.to(DT[dtype]), k.to(DT[dtype]), v, scale=1.0) == 0).all()
+
+
 CACHED = [  # T, heads, kv_heads, kv_len, q_len, window, sinks, page
     (1, 2, 2, [1, 0, 31], None, 0, 0, 32),
     (1, 8, 2, [33, 300, 64], None, 0, 0, 64),
