@@ -145,7 +145,9 @@ void kv_attention_kernel(AttnParams p) {
         qh[mt][j][k] = hi;
         if constexpr (kTwo) ql[mt][j][k] = (_Float16)(y - (float)hi);
       }
-    cs[mt] = p.cs * __builtin_ldexpf(1.0f, e);
+    // kept within fp32: 0 would make NaN of a hidden score, infinity of a score of
+    // 0; past the ends scores are 0, or too far apart for two weights, all the same
+    cs[mt] = fminf(fmaxf(p.cs * __builtin_ldexpf(1.0f, e), 1.17549435e-38f), 3.402823466e38f);
   }
 
   float m[MT], l[MT];

@@ -514,6 +514,29 @@ def test_kv_attention_queries_of_all_sizes_and_strides():
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_scales_that_leave_the_range_of_fp32_with_a_rows_size(dtype):
+    D, lens = 64, [90]
+    pg = Paged(lens, 2, D, 32)
+    k, v = rand(2, 1, 90, 2, D) * 1e-3, rand(3, 1, 90, 2, D)
+    A.kv_write(pg.pool, pg.pages, k, v, ints([0]))
+    ko, vo = torch.zeros_like(k), torch.zeros_like(v)
+    A.kv_read(pg.pool, pg.pages, ints([0]), ko, vo)
+    q = rand(5, 1, 3, 4, D, dtype=dtype)
+    tiny = (q.float() * 2.0 ** -125).to(q.dtype)
+    for scale in (1e-10, 1e-30):  # scores of 0: means
+        check(A.kv_attention(pg.pool, pg.pages, tiny, ints(lens), scale=scale), tiny, ko, vo, [3], lens, scale, True, 0, 0,
+              dtype, True)
+    huge = torch.zeros_like(q)
+    huge[..., 5] = 1e36  # the largest key of channel 5 alone
+    got = host(A.kv_attention(pg.pool, pg.pages, huge, ints(lens), scale=1000.0))
+    for i in range(3):
+        for h in range(4):
+            x = host(ko)[0, :88 + i, h // 2, 5]
+            want = host(vo)[0, :88 + i, h // 2][x == x.max()].mean(0)
+            assert (np.abs(got[0, i, h] - want) <= np.abs(want) * 2.0 ** -8 + 2.0 ** -10).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("window, sinks", [(0, 0), (6, 2)])
 def test_kv_attention_unseen_tokens_may_be_odd_and_pages_gone(dtype, window, sinks):
     D, T, n = 64, 6, 100
