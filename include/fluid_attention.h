@@ -86,7 +86,7 @@ typedef struct {
  * whatever its key and value hold.  Scores times log2(e) are held in fp32: past
  * 2.3e38 a score is infinite. */
 typedef struct {
-  float scale; /* positive, finite */
+  float scale; /* positive, at most 2^127 */
   int32_t causal;
   int32_t window; /* 0: none */
   int32_t sinks;  /* first tokens that stay visible beside the window */

@@ -2,7 +2,6 @@
 #include "fluid_attention.h"
 
 #include <algorithm>
-#include <cmath>
 #include <cstdint>
 
 #include "../host/handles.h"
@@ -143,7 +142,8 @@ void set_workspace(AttnParams& p, int head_dim, void* ws, uint64_t bytes) {
 
 AttnParams check_opts(const fluid_attention_opts* o, const fluid_tokens* qd, int kv_heads) {
   require(o != nullptr, "opts: NULL");
-  require(std::isfinite(o->scale) && o->scale > 0.0f, "opts: scale must be positive and finite");
+  // times log2(e) it still is a number; a NaN fails both
+  require(o->scale > 0.0f && o->scale <= 0x1p127f, "opts: scale must be positive and at most 2^127");
   require(o->causal == 0 || o->causal == 1, "opts: causal must be 0 or 1");
   require(o->window >= 0 && o->sinks >= 0, "opts: window and sinks must not be negative");
   require(qd->heads % kv_heads == 0, "q: heads must be a multiple of kv_heads");

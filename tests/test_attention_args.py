@@ -119,6 +119,14 @@ def test_attention_refusals(bad, word):
         assert st == INVALID and word in msg, (st, msg)
 
 
+def test_scales_whose_log2_form_is_no_number_are_refused():
+    for call in (kv, dense):
+        assert call(o=opts(scale=2.0 ** 127))[0] == UNSUPPORTED
+        for scale in (2.4e38, 3.4e38):  # times log2(e): past fp32
+            st, msg = call(o=opts(scale=scale))
+            assert st == INVALID and "scale" in msg, (st, msg)
+
+
 def test_more_refusals():
     for st, msg, word in ((*kv(o=opts(causal=0)), "causal"), (*kv(kv_max=0), "kv_max"), (*kv(kv_len=None), "kv_len"),
                           (*kv(pool=ADDR + 4), "aligned"), (*dense(k=None), "NULL"),
