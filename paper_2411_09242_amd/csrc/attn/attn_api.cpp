@@ -3,6 +3,7 @@
 
 #include <algorithm>
 #include <cstdint>
+#include <initializer_list>
 
 #include "../host/handles.h"
 #include "../host/kparams.h"
@@ -13,7 +14,15 @@ namespace fluid {
 namespace {
 
 constexpr int64_t kMostTokens = int64_t(1) << 30;  // positions and windows stay within int32 sums
-constexpr int64_t kMostGroups = (int64_t(1) << 31) - 1;
+constexpr int64_t kMostThreads = (int64_t(1) << 32) - 1;  // of a launch
+
+// A product of counts, or more than any launch or index can hold.
+int64_t product(std::initializer_list<int64_t> counts) {
+  int64_t n = 1;
+  for (int64_t c : counts)
+    if (__builtin_mul_overflow(n, c, &n)) return int64_t(1) << 62;
+  return n;
+}
 
 void check_head_dim(int d) { require(d == 32 || d == 64 || d == 128, "head_dim must be 32, 64 or 128"); }
 
@@ -101,8 +110,8 @@ void kv_io(const fluid_kv_cache* cache, const void* pool, const int32_t* pages, 
   p.tokens = kd->tokens;
   const int span = write ? 8 : kKvTile;
   p.runs = (kd->tokens + span - 2) / span + 1;
-  p.items = int64_t(cache->batch) * p.runs * cache->kv_heads;
-  require(p.items < kMostGroups, "k, v: too large for one launch");
+  p.items = product({cache->batch, p.runs, cache->kv_heads});  // a wavefront each
+  require(p.items <= kMostThreads / 64 - 3, "k, v: too large for one launch");  // four to a workgroup
   p.div_heads = make_fastdiv(cache->kv_heads);
   p.div_runs = make_fastdiv(p.runs);
   run_kv_io(p, kd->dtype, cache->head_dim, write, stream);
@@ -114,18 +123,21 @@ void kv_io(const fluid_kv_cache* cache, const void* pool, const int32_t* pages, 
 // shares of at least `least` steps.
 void plan_shares(AttnParams& p, int64_t visible, int64_t slots, int64_t least) {
   p.row_tiles = (int32_t)((int64_t(p.q_tokens) * p.group + p.row_tile - 1) / p.row_tile);
-  const int64_t items = int64_t(p.batch) * p.kv_heads * p.row_tiles;
+  const int64_t items = product({p.batch, p.kv_heads, p.row_tiles});
+  require(items <= kMostThreads / 64 && product({p.batch, p.kv_heads, p.q_tokens, p.group}) < int64_t(1) << 31,
+          "q: too large for one launch");
   const int64_t steps = visible / p.token_tile + 1;
   // a row's shares are put together by one workgroup: 507 of them took 4 us more than 254
   const int64_t splits = std::max<int64_t>(1, std::min({slots / items, steps / least, (int64_t)256}));
   p.chunk = (int32_t)((steps + splits - 1) / splits);
   p.splits = (int32_t)((steps + p.chunk - 1) / p.chunk);
-  require(items * p.splits < kMostGroups && int64_t(p.batch) * p.kv_heads * p.q_tokens * p.group < kMostGroups,
-          "q: too large for one launch");
   p.div_group = make_fastdiv(p.group);
   p.div_tiles = make_fastdiv(p.row_tiles);
   p.div_heads = make_fastdiv(p.kv_heads);
   p.div_splits = make_fastdiv(p.splits);
+}
+void check_launch(const AttnParams& p, int threads) {
+  require(product({p.batch, p.kv_heads, p.row_tiles, p.splits, threads}) <= kMostThreads, "q: too large for one launch");
 }
 uint64_t workspace_of(const AttnParams& p, int head_dim) {
   return p.splits == 1 ? 0 : uint64_t(p.batch) * p.kv_heads * p.row_tiles * p.splits * p.row_tile * (head_dim + 2) * 4;
@@ -198,6 +210,7 @@ AttnParams plan_kv_attention(const fluid_kv_cache* cache, const fluid_attention_
     plan_shares(p, visible, 1, 1);
     p.waves = many;
   }
+  check_launch(p, 64 * p.waves);
   return p;
 }
 AttnParams plan_attention(const fluid_attention_opts* opts, const fluid_tokens* qd, const fluid_tokens* kd) {
@@ -236,6 +249,7 @@ AttnParams plan_attention(const fluid_attention_opts* opts, const fluid_tokens* 
   p.levels = (int32_t)std::min<int64_t>(places, kMostLevels) + p.row_tiles + 1;
   if (p.splits == 1 && groups > 256 && heads / p.rank_step <= 64) p.rank_heads = (int32_t)(heads / p.rank_step);
   p.div_head = make_fastdiv(p.row_tiles * p.splits);
+  check_launch(p, 256 * p.teams);
   return p;
 }
 
@@ -251,7 +265,9 @@ fluid_status fluid_kv_pool_bytes(const fluid_kv_cache* cache, uint64_t* bytes) {
   return call_guarded([&] {
     check_cache(cache);
     require(bytes != nullptr, "bytes: NULL");
-    *bytes = uint64_t(cache->n_pages) * cache->kv_heads * block_bytes(cache);
+    const int64_t n = product({cache->n_pages, cache->kv_heads, block_bytes(cache)});
+    require(n < int64_t(1) << 62, "cache: too large");
+    *bytes = n;
   });
 }
 

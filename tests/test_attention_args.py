@@ -127,6 +127,32 @@ def test_scales_whose_log2_form_is_no_number_are_refused():
             assert st == INVALID and "scale" in msg, (st, msg)
 
 
+def test_what_no_launch_can_hold_is_refused():
+    """A launch has fewer than 2^32 threads: 256 (or more) to four octets of
+    tokens, to 128 rows of a kv head, to 16 rows over the cache."""
+    def many(batch, tokens_=1, heads=128):  # one token's data for all
+        return tokens(batch=batch, tokens=tokens_, heads=heads, head_dim=32, stride=(0, 0, 0))
+
+    def out(batch, heads=128):
+        return tokens(batch=batch, tokens=1, heads=heads, head_dim=32, stride=(32 * heads, 32, 32))
+    for batch, st_ in ((1 << 17, UNSUPPORTED), (1 << 20, INVALID)):  # 2^24 and 2^27 octets
+        c = cache(kv_heads=128, head_dim=32, batch=batch)
+        st, msg = io(c=c, kd=many(batch), vd=many(batch))
+        assert st == st_ and ("too large" in msg) == (st_ == INVALID), (batch, st, msg)
+    for batch, st_ in ((1 << 16, UNSUPPORTED), (1 << 18, INVALID)):  # 2^23 and 2^25 kv heads
+        c = cache(kv_heads=128, head_dim=32, batch=batch)
+        for st, msg in (kv(c=c, qd=many(batch), od=out(batch)), dense(qd=many(batch), kd=many(batch), vd=many(batch), od=out(batch))):
+            assert st == st_ and ("too large" in msg) == (st_ == INVALID), (batch, st, msg)
+    most = (1 << 31) - 1  # counts whose product is past 64 bits
+    c = cache(kv_heads=most, head_dim=32, batch=most)
+    q = tokens(batch=most, tokens=1 << 30, heads=most, head_dim=32, stride=(0, 0, 0))
+    o = tokens(batch=most, tokens=1 << 30, heads=most, head_dim=32, stride=(1 << 40, 1 << 40, 32))
+    for st, msg in (io(c=c, kd=q, vd=q), kv(c=c, qd=q, od=o), dense(qd=q, kd=q, vd=q, od=o)):
+        assert st == INVALID and "too large" in msg, (st, msg)
+    c, n = cache(kv_heads=most, n_pages=most), C.c_uint64()
+    assert A._lib().fluid_kv_pool_bytes(ref(c), C.byref(n)) == INVALID
+
+
 def test_more_refusals():
     for st, msg, word in ((*kv(o=opts(causal=0)), "causal"), (*kv(kv_max=0), "kv_max"), (*kv(kv_len=None), "kv_len"),
                           (*kv(pool=ADDR + 4), "aligned"), (*dense(k=None), "NULL"),
