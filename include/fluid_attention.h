@@ -138,8 +138,9 @@ fluid_status fluid_kv_attention(const fluid_kv_cache* cache, const void* pool, c
  * Arithmetic: on the bf16 matrix cores with fp32 sums, softmax in fp32.  bf16:
  * a weight is rounded to bf16 for its product with the value, and so summed.
  * fp32: operands are three bf16 parts each, which leaves the error of an fp32
- * product; magnitudes from 3.3895e38 on, beyond bf16's largest, count as
- * infinite.  Workspace and errors as fluid_kv_attention. */
+ * product; a row's sums run before their division, with weights of up to 2^8, and
+ * overflow to infinity for values near fp32's largest.  Workspace and errors as
+ * fluid_kv_attention. */
 fluid_status fluid_attention_workspace(const fluid_attention_opts* opts, const fluid_tokens* qd,
                                        const fluid_tokens* kd, uint64_t* bytes);
 fluid_status fluid_attention(const fluid_attention_opts* opts, const fluid_tokens* qd, const void* q,

@@ -23,14 +23,20 @@ namespace {
 
 constexpr int BN = kF32Tile;
 
-// Two values' parts, packed: the first in the low halves.
+// Two values' parts, packed: the first in the low halves.  Past bf16's largest a
+// first part rounds to infinity; `cut` takes such a value's upper bits as they are.
+// What the first part leaves is added to `odd` as 0, or as NaN where it is none.
 struct Parts {
   uint32_t h, m, l;
 };
-__device__ __forceinline__ Parts split2(float a, float b) {
+template <bool CUT>
+__device__ __forceinline__ Parts split2(float a, float b, float& odd) {
   Parts r;
   r.h = pack_bf16(a, b);
+  if (CUT && (r.h & 0x7f80u) == 0x7f80u) r.h = (r.h & 0xffff0000u) | (__float_as_uint(a) >> 16);
+  if (CUT && (r.h & 0x7f800000u) == 0x7f800000u) r.h = (r.h & 0xffffu) | (__float_as_uint(b) & 0xffff0000u);
   const float am = a - __uint_as_float(r.h << 16), bm = b - __uint_as_float(r.h & 0xffff0000u);
+  odd = __builtin_fmaf(bm, 0.0f, __builtin_fmaf(am, 0.0f, odd));
   r.m = pack_bf16(am, bm);
   r.l = pack_bf16(am - __uint_as_float(r.m << 16), bm - __uint_as_float(r.m & 0xffff0000u));
   return r;
@@ -38,13 +44,18 @@ __device__ __forceinline__ Parts split2(float a, float b) {
 // Eight values' parts as operands.
 struct Split8 {
   piece h, m, l;
-  __device__ __forceinline__ explicit Split8(const float* x) {
+  float odd = 0.0f;
+  template <bool CUT>
+  __device__ __forceinline__ void split(const float* x) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const Parts r = split2(x[2 * i], x[2 * i + 1]);
+      const Parts r = split2<CUT>(x[2 * i], x[2 * i + 1], odd);
       h[i] = r.h, m[i] = r.m, l[i] = r.l;
     }
   }
+  __device__ __forceinline__ explicit Split8(const float* x) { split<false>(x); }
+  // some value is an infinity, a NaN or past bf16's largest
+  __device__ __forceinline__ bool past() const { return odd != odd; }
 };
 __device__ __forceinline__ v8i16 op(piece x) { return __builtin_bit_cast(v8i16, x); }
 
@@ -71,7 +82,8 @@ void attention_f32_kernel(AttnParams p) {
     float x[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = w.q[16 * s + 8 * half + e];
-    const Split8 r(x);
+    Split8 r(x);
+    if (r.past()) r.split<true>(x);
     qh[s] = op(r.h), qm[s] = op(r.m), ql[s] = op(r.l);
   }
 
@@ -98,17 +110,20 @@ void attention_f32_kernel(AttnParams p) {
       const int at = tid + kTeam * i;
       const bool values = kTeam * i + 64 * w.wave >= PIECES;
       const int x = at % PIECES, t = x / PPR, c = x % PPR;
-      float f[8], odd = 0.0f;
+      float f[8];
       raw[i].floats(f);
+      Split8 r(f);
+      if (r.past()) {
+        bool odd = false;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) odd = __builtin_fmaf(f[e], 0.0f, odd);
-      if (odd != odd) {
-        if (values) dirty = true;
-        else odd_key = true;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = odd_value(f[e]) ? 0.0f : f[e];
+        for (int e = 0; e < 8; ++e) {
+          odd |= odd_value(f[e]);
+          f[e] = odd_value(f[e]) ? 0.0f : f[e];
+        }
+        if (values) dirty |= odd;
+        else odd_key |= odd;
+        r.split<true>(f);
       }
-      const Split8 r(f);
       uint16_t* const dst = values ? to.v + At::v(t, c) : to.k + At::k(t, c);
       *(piece*)dst = r.h;
       *(piece*)(dst + PLANE) = r.m;

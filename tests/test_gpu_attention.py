@@ -433,6 +433,65 @@ def test_scores_down_to_the_lowest_are_seen():
         assert (A.attention(q.to(DT[dtype]), k.to(DT[dtype]), v, scale=1.0) == 0).all()
 
 
+TOP = 3.4028234663852886e38
+
+
+@pytest.mark.parametrize("value", [TOP, -TOP, 3.3962e38, -3.3962e38, 3.39e38, float("inf")])
+@pytest.mark.parametrize("T, N, causal, window, sinks", [(150, 150, True, 9, 2), (150, 150, True, 0, 0), (3, 100, True, 0, 0),
+                                                        (150, 150, False, 9, 2)])
+def test_fp32_values_and_keys_to_the_end_of_the_range(value, T, N, causal, window, sinks):
+    """Past bf16's largest.  A row that does not see them is as without them; a
+    row that does has their weighted value, or overflows: 2^8 is the largest
+    weight before the division."""
+    D, at = 64, N - 40
+    kw = dict(causal=causal, window=window, sinks=sinks)
+    q, k, v = rand(0, 1, T, 2, D), rand(1, 1, N, 2, D), rand(2, 1, N, 2, D)
+    clean = host(A.attention(q, k, v, **kw))
+    v2 = v.clone()
+    v2[0, at, 1, 7] = value
+    got = host(A.attention(q, k, v2, **kw))
+    for i in range(T):
+        rest = np.array_equal(np.delete(got[0, i, 1], 7), np.delete(clean[0, i, 1], 7))
+        assert rest and np.array_equal(got[0, i, 0], clean[0, i, 0])
+        if not OA.sees(N - T + i, at, N, causal, window, sinks):
+            assert got[0, i, 1, 7] == clean[0, i, 1, 7]
+            continue
+        p = host(k)[0, :, 1] @ host(q)[0, i, 1] * D ** -0.5
+        see = [OA.sees(N - T + i, j, N, causal, window, sinks) for j in range(N)]
+        p = np.exp(np.where(see, p, -np.inf) - p[see].max())
+        want = p[at] / p.sum() * value
+        x = got[0, i, 1, 7]
+        assert np.isinf(want) and x == want or abs(x - want) <= 1e-4 * abs(want) or (np.isinf(x) and x * want > 0), (i, x, want)
+    if np.isinf(value):
+        return
+    # as a key: |q| of a quarter there, so that no score overflows
+    q[..., 5] = torch.where(q[..., 5] > 0, 0.25, -0.25)
+    k2 = k.clone()
+    k2[0, at, :, 5] = value
+    got = host(A.attention(q, k2, v, **kw))
+    for i in range(T):
+        for h in range(2):
+            see = np.array([OA.sees(N - T + i, j, N, causal, window, sinks) for j in range(N)])
+            if see[at] and host(q)[0, i, h, 5] * value > 0:
+                assert np.allclose(got[0, i, h], host(v)[0, at, h], rtol=2.0 ** -22)
+            else:
+                see[at] = False
+                x = host(k)[0, see, h] @ host(q)[0, i, h] * D ** -0.5
+                x = np.exp(x - x.max())
+                assert np.allclose(got[0, i, h], x / x.sum() @ host(v)[0, see, h], atol=1e-4)
+
+
+def test_fp32_queries_to_the_end_of_the_range():
+    D, N = 64, 100
+    q, k, v = torch.zeros(1, N, 1, D, device="cuda"), torch.zeros(1, N, 1, D, device="cuda"), rand(1, 1, N, 1, D)
+    k[0, :, 0, 5] = (1 + torch.arange(N, device="cuda")) / 128
+    for value in (TOP, -TOP, 3.3962e38):
+        q[..., 5] = value
+        got = A.attention(q, k, v)
+        want = v if value > 0 else v[:, :1].expand(1, N, 1, D)
+        assert ((got - want).abs() <= want.abs() * 2.0 ** -20).all()
+
+
 CACHED = [  # T, heads, kv_heads, kv_len, q_len, window, sinks, page
     (1, 2, 2, [1, 0, 31], None, 0, 0, 32),
     (1, 8, 2, [33, 300, 64], None, 0, 0, 64),
