@@ -9,7 +9,8 @@
  * are validated before any HIP call, all device memory (pool, tensors, page
  * table, lengths, workspace) is the caller's, nothing is allocated, and a
  * call only enqueues kernels on `hip_stream`, so it can be captured in a HIP
- * graph.  Nothing is kept between calls.  The host-only library validates
+ * graph.  The calling thread's current device has to be the stream's and the
+ * memory's.  Nothing is kept between calls.  The host-only library validates
  * alike and then returns FLUID_E_UNSUPPORTED.
  *
  * Tensors of tokens are [batch, tokens, heads, head_dim] with any strides and

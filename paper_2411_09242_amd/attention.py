@@ -165,6 +165,24 @@ except ImportError:
         return _stream(None, device)
 
 
+try:
+    from torch._C import _cuda_getDevice as _current_device
+except ImportError:
+    def _current_device():
+        return _torch().cuda.current_device()
+
+
+def _launch(f, device, *args):
+    """f(*args) with the tensors' GPU as the current one, as launches need it."""
+    if _current_device() == device:
+        st = f(*args)
+    else:
+        with _torch().cuda.device(device):
+            st = f(*args)
+    if st:
+        fluid._check(st)
+
+
 def _addr(d):
     return C.addressof(d)
 
@@ -193,11 +211,9 @@ def _io(write, pool, pages, k, v, start, count, stream):
     if made is None:
         made = _keep(key, _io_call(pool, pages, k, v, start, count))
     lib, dev, c, kd, vd, _ = made
-    st = (lib.fluid_kv_write if write else lib.fluid_kv_read)(
-        c, pool.data_ptr(), pages.data_ptr(), kd, k.data_ptr(), vd, v.data_ptr(), start.data_ptr(),
-        None if count is None else count.data_ptr(), _raw_stream(dev) if stream is None else _stream(stream, dev))
-    if st:
-        fluid._check(st)
+    _launch(lib.fluid_kv_write if write else lib.fluid_kv_read, dev,
+            c, pool.data_ptr(), pages.data_ptr(), kd, k.data_ptr(), vd, v.data_ptr(), start.data_ptr(),
+            None if count is None else count.data_ptr(), _raw_stream(dev) if stream is None else _stream(stream, dev))
 
 
 def kv_write(pool, pages, k, v, start, count=None, stream=None):
@@ -273,12 +289,10 @@ def kv_attention(pool, pages, q, kv_len, q_len=None, kv_max=None, scale=None, wi
         made = _keep(key, _kv_call(pool, pages, q, kv_len, q_len, kv_max, scale, window, sinks, out))
     lib, dev, c, o, kv_max, qd, od, need, _ = made
     keep, ws, ws_bytes = _workspace(need, workspace, dev, stream) if need else (None, None, 0)
-    st = lib.fluid_kv_attention(
-        c, pool.data_ptr(), pages.data_ptr(), o, kv_max, qd, q.data_ptr(), None if q_len is None else q_len.data_ptr(),
-        kv_len.data_ptr(), od, out.data_ptr(), ws, ws_bytes, _raw_stream(dev) if stream is None else _stream(stream, dev))
+    _launch(lib.fluid_kv_attention, dev,
+            c, pool.data_ptr(), pages.data_ptr(), o, kv_max, qd, q.data_ptr(), None if q_len is None else q_len.data_ptr(),
+            kv_len.data_ptr(), od, out.data_ptr(), ws, ws_bytes, _raw_stream(dev) if stream is None else _stream(stream, dev))
     del keep
-    if st:
-        fluid._check(st)
     return out
 
 
@@ -326,13 +340,11 @@ def attention(q, k, v, q_len=None, kv_len=None, scale=None, causal=True, window=
         made = _keep(key, _dense_call(q, k, v, q_len, kv_len, scale, causal, window, sinks, out))
     lib, dev, o, qd, kd, vd, od, need, _ = made
     keep, ws, ws_bytes = _workspace(need, workspace, dev, stream) if need else (None, None, 0)
-    st = lib.fluid_attention(
-        o, qd, q.data_ptr(), kd, k.data_ptr(), vd, v.data_ptr(), None if q_len is None else q_len.data_ptr(),
-        None if kv_len is None else kv_len.data_ptr(), od, out.data_ptr(), ws, ws_bytes,
-        _raw_stream(dev) if stream is None else _stream(stream, dev))
+    _launch(lib.fluid_attention, dev,
+            o, qd, q.data_ptr(), kd, k.data_ptr(), vd, v.data_ptr(), None if q_len is None else q_len.data_ptr(),
+            None if kv_len is None else kv_len.data_ptr(), od, out.data_ptr(), ws, ws_bytes,
+            _raw_stream(dev) if stream is None else _stream(stream, dev))
     del keep
-    if st:
-        fluid._check(st)
     return out
 
 

@@ -230,6 +230,31 @@ def test_binding_refuses_tensors_that_cannot_be_right():
             A._describe_opts(None, True, window, sinks, 64)
 
 
+def test_calls_run_with_their_tensors_gpu_current(monkeypatch):
+    """A default stream's handle is 0 on every GPU: without this the kernels of
+    tensors on GPU 1 would run on GPU 0."""
+    torch = pytest.importorskip("torch")
+    at, seen = [0], []
+
+    class On:
+        def __init__(self, device):
+            self.device = device
+
+        def __enter__(self):
+            self.was, at[0] = at[0], self.device
+
+        def __exit__(self, *_):
+            at[0] = self.was
+    monkeypatch.setattr(torch.cuda, "device", On)
+    monkeypatch.setattr(A, "_current_device", lambda: at[0])
+    for device in (1, 0):
+        A._launch(lambda *a: seen.append((at[0], a)) or 0, device, 5, 6)
+    assert seen == [(1, (5, 6)), (0, (5, 6))] and at == [0]
+    with pytest.raises(F.FluidError):
+        A._launch(lambda: INVALID, 1)
+    assert at == [0]
+
+
 # ------------------------------------------------------- pins of the oracle
 def test_quantised_values_are_near_and_exact_where_they_can_be():
     rng = np.random.default_rng(1)
