@@ -14,7 +14,7 @@ or bf16 on the GPU, with any strides and contiguous channels; lengths, starts
 and page tables are int32 tensors on the GPU.  Calls enqueue kernels on
 torch's current stream, or on ``stream`` (a torch stream or a raw handle), and
 return without waiting; arguments that cannot be right raise ``FluidError``
-before anything is launched.  What a window has left behind may be freed: page
+before anything is launched, and so do tensors that want gradients.  What a window has left behind may be freed: page
 table entries outside the pool hold no tokens.
 """
 from __future__ import annotations
@@ -146,6 +146,12 @@ def _keep(key, made):
     return made
 
 
+def _check_grad(*tensors):
+    """Refuses tensors that want gradients, which no call here computes."""
+    if any(t.requires_grad for t in tensors) and _torch().is_grad_enabled():
+        _refuse("a tensor requires gradients, and there is no backward pass: detach it, or call under torch.no_grad()")
+
+
 def _device_of(t, name):
     if not t.is_cuda:
         _refuse(f"{name}: a tensor on the GPU is needed, got {t.device}")
@@ -204,6 +210,7 @@ def _io_call(pool, pages, k, v, start, count):
 
 
 def _io(write, pool, pages, k, v, start, count, stream):
+    _check_grad(k, v)
     key = (fluid._lib, pool.shape, pool.stride(), pool.dtype, pool.get_device(), pages.shape, pages.stride(), pages.dtype,
            pages.get_device(), k.dtype, k.shape, k.stride(), k.get_device(), v.dtype, v.shape, v.stride(),
            v.get_device(), _form(start), None if count is None else _form(count))
@@ -279,6 +286,7 @@ def kv_attention(pool, pages, q, kv_len, q_len=None, kv_max=None, scale=None, wi
     are left as they are; allocated as zeros by default).  Returns out."""
     if out is None:
         out = _zeros(q, stream)
+    _check_grad(q, out)
     key = (fluid._lib, pool.shape, pool.stride(), pool.dtype, pool.get_device(), pages.shape, pages.stride(), pages.dtype,
            pages.get_device(), q.dtype, q.shape, q.stride(), q.get_device(), out.dtype, out.shape, out.stride(),
            out.get_device(), _form(kv_len), None if q_len is None else _form(q_len), kv_max, scale, window, sinks)
@@ -331,6 +339,7 @@ def attention(q, k, v, q_len=None, kv_len=None, scale=None, causal=True, window=
     ``kv_attention`` does."""
     if out is None:
         out = _zeros(q, stream)
+    _check_grad(q, k, v, out)
     key = (fluid._lib, q.dtype, q.shape, q.stride(), q.get_device(), k.dtype, k.shape, k.stride(), k.get_device(),
            v.dtype, v.shape, v.stride(), v.get_device(), out.dtype, out.shape, out.stride(), out.get_device(),
            None if q_len is None else _form(q_len), None if kv_len is None else _form(kv_len), scale, causal, window,

@@ -255,6 +255,24 @@ def test_calls_run_with_their_tensors_gpu_current(monkeypatch):
     assert at == [0]
 
 
+def test_tensors_that_want_gradients_are_refused():
+    """There is no backward pass: the result would be detached without a word."""
+    torch = pytest.importorskip("torch")
+    x, want = torch.zeros(1, 4, 2, 64), torch.zeros(1, 4, 2, 64, requires_grad=True)
+    pages, one = torch.zeros(1, 2, dtype=torch.int32), torch.zeros(1, dtype=torch.int32)
+    pool = torch.zeros(2, 2, A.pool_block(32, 64), dtype=torch.uint8)
+    calls = [lambda a, b: A.attention(a, b, b), lambda a, b: A.attention(b, a, b), lambda a, b: A.attention(b, b, a),
+             lambda a, b: A.attention(b, b, b, out=a), lambda a, b: A.kv_attention(pool, pages, a, one),
+             lambda a, b: A.kv_attention(pool, pages, b, one, out=a), lambda a, b: A.kv_write(pool, pages, a, b, one),
+             lambda a, b: A.kv_write(pool, pages, b, a, one), lambda a, b: A.kv_read(pool, pages, one, a, b),
+             lambda a, b: A.kv_read(pool, pages, one, b, a)]
+    for call in calls:
+        with pytest.raises(F.FluidError, match="gradient"):
+            call(want, x)
+        with torch.no_grad(), pytest.raises(F.FluidError, match="GPU"):  # on to the next check
+            call(want, x)
+
+
 # ------------------------------------------------------- pins of the oracle
 def test_quantised_values_are_near_and_exact_where_they_can_be():
     rng = np.random.default_rng(1)
