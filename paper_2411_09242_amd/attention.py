@@ -13,7 +13,9 @@ Tensors of tokens are torch tensors [batch, tokens, heads, head_dim] in fp32
 or bf16 on the GPU, with any strides and contiguous channels; lengths, starts
 and page tables are int32 tensors on the GPU.  Calls enqueue kernels on
 torch's current stream, or on ``stream`` (a torch stream or a raw handle), and
-return without waiting; arguments that cannot be right raise ``FluidError``
+return without waiting.  With ``stream`` the caller orders the call behind what
+makes its tensors and before what uses the result (``wait_stream``); the tensors'
+memory is not handed out again before the call has run.  Arguments that cannot be right raise ``FluidError``
 before anything is launched, and so do tensors that want gradients.  What a window has left behind may be freed: page
 table entries outside the pool hold no tokens.
 """
@@ -158,6 +160,19 @@ def _device_of(t, name):
     return t.get_device()
 
 
+def _as_stream(stream, device):
+    return stream if hasattr(stream, "cuda_stream") else _torch().cuda.ExternalStream(stream, device=device)
+
+
+def _record(stream, device, *tensors):
+    """Keeps tensors that their owner drops until `stream` is done with them:
+    torch hands memory out again in the order of its own stream alone."""
+    s = _as_stream(stream, device)
+    for t in tensors:
+        if t is not None:
+            t.record_stream(s)
+
+
 def _stream(stream, device):
     if stream is None:
         return _torch().cuda.current_stream(device).cuda_stream
@@ -221,6 +236,8 @@ def _io(write, pool, pages, k, v, start, count, stream):
     _launch(lib.fluid_kv_write if write else lib.fluid_kv_read, dev,
             c, pool.data_ptr(), pages.data_ptr(), kd, k.data_ptr(), vd, v.data_ptr(), start.data_ptr(),
             None if count is None else count.data_ptr(), _raw_stream(dev) if stream is None else _stream(stream, dev))
+    if stream is not None:
+        _record(stream, dev, pool, pages, k, v, start, count)
 
 
 def kv_write(pool, pages, k, v, start, count=None, stream=None):
@@ -245,8 +262,7 @@ def _workspace(need, workspace, device, stream):
         if stream is None:
             workspace = torch.empty(need, dtype=torch.uint8, device=device)
         else:
-            s = stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(stream, device=device)
-            with torch.cuda.stream(s):
+            with torch.cuda.stream(_as_stream(stream, device)):
                 workspace = torch.empty(need, dtype=torch.uint8, device=device)
     elif workspace.get_device() != device or not workspace.is_contiguous():
         _refuse(f"workspace: a contiguous tensor on GPU {device} is needed")
@@ -300,6 +316,8 @@ def kv_attention(pool, pages, q, kv_len, q_len=None, kv_max=None, scale=None, wi
     _launch(lib.fluid_kv_attention, dev,
             c, pool.data_ptr(), pages.data_ptr(), o, kv_max, qd, q.data_ptr(), None if q_len is None else q_len.data_ptr(),
             kv_len.data_ptr(), od, out.data_ptr(), ws, ws_bytes, _raw_stream(dev) if stream is None else _stream(stream, dev))
+    if stream is not None:
+        _record(stream, dev, pool, pages, q, q_len, kv_len, out, workspace)
     del keep
     return out
 
@@ -309,8 +327,7 @@ def _zeros(q, stream):
     torch = _torch()
     if stream is None or not q.is_cuda:
         return torch.zeros(q.shape, dtype=q.dtype, device=q.device)
-    s = stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(stream, device=q.device)
-    with torch.cuda.stream(s):
+    with torch.cuda.stream(_as_stream(stream, q.device)):
         return torch.zeros(q.shape, dtype=q.dtype, device=q.device)
 
 
@@ -353,6 +370,8 @@ def attention(q, k, v, q_len=None, kv_len=None, scale=None, causal=True, window=
             o, qd, q.data_ptr(), kd, k.data_ptr(), vd, v.data_ptr(), None if q_len is None else q_len.data_ptr(),
             None if kv_len is None else kv_len.data_ptr(), od, out.data_ptr(), ws, ws_bytes,
             _raw_stream(dev) if stream is None else _stream(stream, dev))
+    if stream is not None:
+        _record(stream, dev, q, k, v, q_len, kv_len, out, workspace)
     del keep
     return out
 

@@ -686,6 +686,34 @@ def test_calls_on_another_stream():
         assert torch.equal(b, A.kv_attention(pg.pool, pg.pages, q, ints([3000]), kv_max=3000))
 
 
+def test_tensors_dropped_behind_a_call_on_another_stream_stay_until_it_has_run():
+    q, k, v = rand(1, 1, 3, 2, 64), rand(2, 1, 3000, 2, 64), rand(3, 1, 3000, 2, 64)
+    pg = Paged([3000], 2, 64, 64)
+    want = A.attention(q, k, v)
+    busy = torch.randn(8192, 8192, device="cuda").bfloat16()
+    s = torch.cuda.Stream()
+    for stream in (s, s.cuda_stream):
+        t = [x.clone() for x in (q, k, v)]
+        at = ints([0])
+        used = {x.data_ptr() for x in (*t, at)}
+        out = torch.zeros_like(q)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(s):
+            for _ in range(8):  # some milliseconds
+                torch.mm(busy, busy)
+        A.attention(*t, out=out, stream=stream)
+        A.kv_write(pg.pool, pg.pages, t[1], t[2], at, stream=stream)
+        del t, at
+        fresh = [torch.full_like(y, float("nan")) for y in (q, k, v)] + [ints([1 << 20])]
+        early = not s.query()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+        assert not early or not used & {y.data_ptr() for y in fresh}
+        ko, vo = torch.zeros_like(k), torch.zeros_like(v)
+        A.kv_read(pg.pool, pg.pages, ints([0]), ko, vo)
+        assert np.array_equal(host(ko)[0, :, 0], OA.values(*OA.quantise(host(k)[0, :, 0].astype(np.float32))))
+
+
 def test_a_captured_decode_step_replays():
     D, H, P, B = 128, 4, 64, 2
     pg = Paged([2000] * B, H, D, P)
