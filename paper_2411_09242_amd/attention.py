@@ -134,6 +134,8 @@ def _describe_opts(scale, causal, window, sinks, head_dim):
 # strides and devices and on its numbers alone, and a decoding loop makes the
 # same few calls over and over: they are made once for each such set.  (Filling
 # and checking them takes 9 us, as long as a small kernel; finding them, 2.)
+# kv_max, which grows from step to step, is no part of the set: it decides the
+# workspace alone, whose size is asked for again where kv_max is another.
 _calls = {}
 
 
@@ -269,7 +271,7 @@ def _workspace(need, workspace, device, stream):
     return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
-def _kv_call(pool, pages, q, kv_len, q_len, kv_max, scale, window, sinks, out):
+def _kv_call(pool, pages, q, kv_len, q_len, scale, window, sinks, out):
     dev = _device_of(pool, "pool")
     qd = _describe(q, "q", dev)
     od = qd if out is None else _describe(out, "out", dev)
@@ -277,16 +279,25 @@ def _kv_call(pool, pages, q, kv_len, q_len, kv_max, scale, window, sinks, out):
     c, o = _describe_cache(pool, pages, D, dev), _describe_opts(scale, True, window, sinks, D)
     _check_ints(kv_len, "kv_len", n, dev)
     _check_ints(q_len, "q_len", n, dev)
-    if kv_max is None:
-        kv_max = c.max_pages * c.page_tokens
-    need = _U64()
-    fluid._check(_lib().fluid_kv_attention_workspace(_addr(c), _addr(o), kv_max, _addr(qd), C.byref(need)))
-    return (_lib(), dev, _addr(c), _addr(o), kv_max, _addr(qd), _addr(od), need.value, (c, o, qd, od))
+    # the last is (kv_max, bytes of workspace) of the latest call
+    return [_lib(), dev, _addr(c), _addr(o), _addr(qd), _addr(od), c.max_pages * c.page_tokens, (c, o, qd, od), (None, 0)]
+
+
+def _kv_need(made, kv_max):
+    """Bytes of workspace for a described call and this bound."""
+    lib, _, c, o, qd, _, _, _, (most, need) = made
+    if most != kv_max:
+        n = _U64()
+        fluid._check(lib.fluid_kv_attention_workspace(c, o, kv_max, qd, C.byref(n)))
+        need = n.value
+        made[8] = kv_max, need
+    return need
 
 
 def kv_attention_workspace(pool, pages, q, kv_max=None, scale=None, window=0, sinks=0):
     """Bytes of workspace that ``kv_attention`` needs for these arguments."""
-    return _kv_call(pool, pages, q, None, None, kv_max, scale, window, sinks, None)[7]
+    made = _kv_call(pool, pages, q, None, None, scale, window, sinks, None)
+    return _kv_need(made, made[6] if kv_max is None else kv_max)
 
 
 def kv_attention(pool, pages, q, kv_len, q_len=None, kv_max=None, scale=None, window=0, sinks=0, out=None,
@@ -305,13 +316,16 @@ def kv_attention(pool, pages, q, kv_len, q_len=None, kv_max=None, scale=None, wi
     _check_grad(q, out)
     key = (fluid._lib, pool.shape, pool.stride(), pool.dtype, pool.get_device(), pages.shape, pages.stride(), pages.dtype,
            pages.get_device(), q.dtype, q.shape, q.stride(), q.get_device(), out.dtype, out.shape, out.stride(),
-           out.get_device(), _form(kv_len), None if q_len is None else _form(q_len), kv_max, scale, window, sinks)
+           out.get_device(), _form(kv_len), None if q_len is None else _form(q_len), scale, window, sinks)
     made = _calls.get(key)
     if made is None:
         if kv_len is None:
             _refuse("kv_len: needed")
-        made = _keep(key, _kv_call(pool, pages, q, kv_len, q_len, kv_max, scale, window, sinks, out))
-    lib, dev, c, o, kv_max, qd, od, need, _ = made
+        made = _keep(key, _kv_call(pool, pages, q, kv_len, q_len, scale, window, sinks, out))
+    lib, dev, c, o, qd, od, most, _, _ = made
+    if kv_max is None:
+        kv_max = most
+    need = _kv_need(made, kv_max)
     keep, ws, ws_bytes = _workspace(need, workspace, dev, stream) if need else (None, None, 0)
     _launch(lib.fluid_kv_attention, dev,
             c, pool.data_ptr(), pages.data_ptr(), o, kv_max, qd, q.data_ptr(), None if q_len is None else q_len.data_ptr(),

@@ -787,6 +787,23 @@ def test_a_refused_append_leaves_the_cache_as_it_was():
     assert c.lengths == [45, 45]
 
 
+def test_a_decoding_loop_describes_its_calls_once():
+    c = A.KvCache(2, 2, 64, 2100, page_tokens=32)
+    k, q = rand(1, 2, 2030, 2, 64, dtype="bf16"), rand(2, 2, 1, 4, 64, dtype="bf16")
+    c.append(k, k)
+    sizes, needs = [], set()
+    for i in range(40):
+        c.append(k[:, :1], k[:, :1])
+        got = c.attend(q)
+        sizes.append(len(A._calls))
+        needs.add(A.kv_attention_workspace(c.pool, c.pages, q, max(c.lengths)))
+        assert torch.equal(got, A.kv_attention(c.pool, c.pages, q, c.kv_len, kv_max=max(c.lengths)))
+    assert len(needs) > 1  # the loop passes a length from which the tokens are split
+    assert sizes[0] == sizes[-1]
+    with pytest.raises(F.FluidError, match="kv_max"):
+        A.kv_attention(c.pool, c.pages, q, c.kv_len, kv_max=0)
+
+
 def test_trim_without_a_window_gives_nothing_back():
     c = A.KvCache(1, 2, 64, 128, page_tokens=32)
     k = rand(1, 1, 100, 2, 64)
