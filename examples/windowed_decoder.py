@@ -107,7 +107,10 @@ class Decoder:
         return x
 
     def prompt(self, x):
-        """The prompt's hidden states; its keys and values go into the cache."""
+        """The prompt's hidden states; its keys and values go into the cache,
+        which has to be empty: ``extend`` takes what comes behind."""
+        if any(n for c in self.caches for n in c.lengths):
+            raise ValueError("a prompt sees its own tokens alone, and the cache holds some: use extend, or clear it")
         def attend(layer, q, k, v, out):
             self.A.attention(q, k, v, window=self.window, sinks=self.sinks, out=out)
             self.caches[layer].append(k, v)

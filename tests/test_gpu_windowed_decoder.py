@@ -78,3 +78,16 @@ def test_command_line(capsys):
     W.main(["--hidden", "256", "--heads", "4", "--kv-heads", "2", "--head-dim", "64", "--ffn", "512", "--prompt", "70",
             "--steps", "4", "--window", "32"])
     assert "last output finite: True" in capsys.readouterr().out
+
+
+def test_a_second_prompt_behind_cached_tokens_is_refused():
+    """It would not see them."""
+    d = make()
+    x = torch.randn(2, 40, 128, device="cuda").bfloat16()
+    first = d.prompt(x).clone()
+    with pytest.raises(ValueError, match="extend"):
+        d.prompt(x)
+    for c in d.caches:
+        assert c.lengths == [40, 40]
+        c.clear(0), c.clear(1)
+    assert torch.equal(d.prompt(x), first)
