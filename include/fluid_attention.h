@@ -30,7 +30,8 @@ extern "C" {
 /* A tensor of tokens.  Channels are contiguous; stride holds the distance in
  * elements between sequences, tokens and heads (not negative; 0 repeats an
  * input; an output's are at least head_dim, and its elements must not
- * overlap).  head_dim is 32, 64 or 128.  Rows that start on 16-byte addresses
+ * overlap).  head_dim is 32, 64 or 128; batch, tokens and heads are at least 1
+ * (a sequence's own lengths may be 0).  Rows that start on 16-byte addresses
  * are fastest; others are read and written element by element. */
 typedef struct {
   int32_t dtype; /* FLUID_F32 or FLUID_BF16 */
@@ -119,12 +120,16 @@ fluid_status fluid_kv_read(const fluid_kv_cache* cache, const void* pool, const 
  * (NULL: T; clamped to [0, T]) and kv_len[b] tokens (clamped to [0, the
  * table's row]), its newest being the queries' own.  Rows from q_len[b] on
  * are left as they are.  kv_max: the largest kv_len the caller expects
- * (>= 1); it only sizes the split of long caches over the GPU, results are
- * right for any kv_len.  workspace: 256-byte aligned device memory of at least
+ * (>= 1); it sizes the split of long caches over the GPU.  Results are right for
+ * any kv_len, but the split is in equal shares of kv_max: caches far shorter are
+ * shared by few workgroups, and slower than with a kv_max near their length.  workspace: 256-byte aligned device memory of at least
  * the bytes fluid_kv_attention_workspace returns for the same arguments (0:
  * NULL will do), for this call alone while it runs.  Arithmetic: products on the
- * f16 matrix cores with fp32 sums (fp32 tensors in two f16 parts each, at the
- * error of an fp32 product), softmax in fp32.  Errors: FLUID_E_INVALID;
+ * f16 matrix cores with fp32 sums, softmax in fp32.  bf16: a query's channels
+ * below 2^-14 of its largest are rounded to 2^-25 of that, and a weight to f16
+ * (11 bits) for its product with the value.  fp32: queries and weights are two
+ * f16 parts each, within 2^-22 of themselves and queries within 2^-25 of the
+ * row's largest: up to four times an fp32 rounding.  Errors: FLUID_E_INVALID;
  * FLUID_E_ARENA_TOO_SMALL (workspace). */
 fluid_status fluid_kv_attention_workspace(const fluid_kv_cache* cache, const fluid_attention_opts* opts,
                                           int32_t kv_max, const fluid_tokens* qd, uint64_t* bytes);

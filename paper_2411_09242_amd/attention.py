@@ -309,7 +309,8 @@ def kv_attention(pool, pages, q, kv_len, q_len=None, kv_max=None, scale=None, wi
     ``window`` tokens up to its own and the first ``sinks`` ones.  scale: of
     q . k, 1 / sqrt(head_dim) by default.  kv_max: the largest kv_len to
     expect, which sizes the split of long caches over the GPU (by default all
-    that a row of the table can name).  out: where to write (rows past q_len
+    that a row of the table can name; caches far shorter than it are slower than
+    with a bound near their length).  out: where to write (rows past q_len
     are left as they are; allocated as zeros by default).  Returns out."""
     if out is None:
         out = _zeros(q, stream)
@@ -395,7 +396,10 @@ class KvCache:
 
     Pages are handed out on the host as sequences grow and given back when a
     window has left them behind (``trim``) or a sequence ends (``clear``).
-    ``lengths`` is the host's copy; ``kv_len`` the device's."""
+    ``lengths`` is the host's copy; ``kv_len`` the device's.  Every change copies
+    the whole table and the lengths to the device, which takes host time in
+    proportion to batch x max_tokens / page_tokens.  Methods run on torch's
+    current stream; ``attend`` takes ``stream``, to be ordered by the caller."""
 
     def __init__(self, batch, kv_heads, head_dim, max_tokens, n_pages=None, page_tokens=64, device="cuda"):
         torch = self.torch = _torch()

@@ -5,12 +5,17 @@
 //
 // 8192 queries of 32 heads of 128 (8 of keys), window 2048: 267 to 292 us (by
 // card), 820 to 900 TFLOP/s of the products needed, where a library product of 8192^3
-// reaches 1140.  MFMA are 47 % and vector instructions 44 % of the cycles, at a
+// reaches 1140.  MFMA are 46 % and vector instructions 44 % of the cycles, at a
 // clock of 1.8 GHz of 2.4: power bounds it.  The products alone, without copies
 // and weights, take 193 us; with LDS operands read further ahead, copies a step
 // and a half ahead behind two barriers, or one of a SIMD's two wavefronts
 // preferred the time is the same or worse.  2048 queries of 32 heads (window
-// 1024) take 42 to 48 us: two workgroups to a compute unit, of 2 to 19 steps each.
+// 1024) take 42 to 50 us: two workgroups to a compute unit, of 2 to 19 steps each.
+//
+// Weights are rounded to bf16, the type that the values' products take: a second
+// part of them would double those products.  That, averaged over the tokens, is
+// below the output's own rounding: the error of 8192 queries against 64 bits is
+// 0.21 % of the output, 0.15 % with fp32 weights.
 #include "attn_rows.h"
 #include "launch_attn.h"
 

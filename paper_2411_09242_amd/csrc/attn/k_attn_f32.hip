@@ -9,11 +9,12 @@
 // MFMA needs eight of 64.  Keys and values are split on their way from memory
 // through registers to LDS, one tile of 32 tokens ahead of the products.
 //
-// 8 sequences of 207 to 512 tokens of 16 heads of 64, both directions: 40 us (42
-// before the longest came first, 61 with the fp32 MFMA).  Vector instructions
-// (exponentials, splits of the weights and of the keys and values that every
-// workgroup loads) are 43 % of the cycles, MFMA 36 %, and two wavefronts a SIMD
-// do not hide all waits; a third spills (8 x 512 causal queries 43 -> 60 us).
+// 8 sequences of up to 512 tokens of 16 heads of 64, both directions: 40 to 44 us
+// by card (42 before the longest came first, 61 with the fp32 MFMA).  Vector
+// instructions (exponentials, splits of the weights and of the keys and values
+// that every workgroup loads) are 37 % of the cycles of a busy compute unit, MFMA
+// 31 %, and two wavefronts a SIMD do not hide all waits; a third spills (44 ->
+// 52 us; 8 x 512 causal queries 45 -> 62).
 #include "attn_rows.h"
 #include "launch_attn.h"
 

@@ -13,9 +13,9 @@
 // (4.5 TB/s; a copy of 4 GiB has 4.7).  Non-temporal stores made the reads of
 // 512 to 1024 tokens 10 % faster and the attention that follows slower (512
 // queries over 8192 tokens and 32 heads, with the read: 161 us, 189 with them).
-// Writing has 25 vector instructions a value, 10 us of the 18.6 that 2048
-// tokens (44 MB) take; all wavefronts of so many fit the GPU at once, so loads
-// and arithmetic overlap little.  One token or 16 take 5 to 6 us: the
+// Writing has some 20 vector instructions a value, 84 % of the cycles of the 13.4
+// us that 2048 tokens (44 MB) take; all wavefronts of so many fit the GPU at once,
+// so loads and arithmetic overlap little.  One token or 16 take 5 to 6 us: the
 // launch and a chain of dependent loads (lengths; the page, beside the values to
 // write; the words to read, or those that keep some of their nibbles).
 #include "kv_tile.h"

@@ -12,21 +12,24 @@
 // a dequantised operand loses nothing.
 //
 // Queries are scaled by a power of two per row before they become f16 (bf16
-// ones then are exact but for what lies 2^-14 below a row's largest); fp32
-// queries and probabilities are two f16 parts each and two products.
+// ones then are exact but for what lies 2^-14 below a row's largest, rounded to
+// 2^-25 of it).  The weights of bf16 queries are rounded to f16: 11 bits, where
+// the output has 8, and half the products of two parts (32 x 8192 tokens: error
+// against 64 bits 0.17 % of the output, as with fp32 weights).  fp32 queries and
+// weights are two f16 parts each and two products: 22 bits.
 //
 // The wavefronts of a workgroup take token tiles in turn and join their sums
 // in LDS; long caches are split over workgroups, joined by a second kernel.
 //
 // Bound by reading the cache once it is long: 131072 tokens of 8 heads of 128,
-// 168 MB, take 31 us (5.4 TB/s; a copy of 4 GiB has 4.7, reads alone up to
-// 7.2) and 4.8 for the join; 32 sequences of 2581 to 8192 tokens, 222 MB, 49.
-// Vector instructions are 59 % of the cycles and MFMA 13 %, so that three
+// 168 MB, take 30 to 32 us (5.4 TB/s; a copy of 4 GiB has 4.7, reads alone up to
+// 7.2) and 5 for the join; 32 sequences of 2581 to 8192 tokens, 222 MB, 48.
+// Vector instructions are 60 % of the cycles and MFMA 13 %, so that three
 // wavefronts a SIMD have to cover the loads; a fourth has 128 registers and
 // spills, a whole tile ahead in registers of its own was slower too.  Short
 // caches are bound by the launch and four dependent loads (lengths, page, keys
 // and values): 8 sequences of up to 1000 tokens of 12 heads of 64 in fp32, up to
-// five queries each, 9.2 us.
+// five queries each, 10 us.
 #include "kv_tile.h"
 #include "launch_attn.h"
 
