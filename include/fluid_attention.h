@@ -122,15 +122,16 @@ fluid_status fluid_kv_read(const fluid_kv_cache* cache, const void* pool, const 
  * are left as they are.  kv_max: the largest kv_len the caller expects
  * (>= 1); it sizes the split of long caches over the GPU.  Results are right for
  * any kv_len, but the split is in equal shares of kv_max: caches far shorter are
- * shared by few workgroups, and slower than with a kv_max near their length.  workspace: 256-byte aligned device memory of at least
- * the bytes fluid_kv_attention_workspace returns for the same arguments (0:
- * NULL will do), for this call alone while it runs.  Arithmetic: products on the
- * f16 matrix cores with fp32 sums, softmax in fp32.  bf16: a query's channels
- * below 2^-14 of its largest are rounded to 2^-25 of that, and a weight to f16
- * (11 bits) for its product with the value.  fp32: queries and weights are two
- * f16 parts each, within 2^-22 of themselves and queries within 2^-25 of the
- * row's largest: up to four times an fp32 rounding.  Errors: FLUID_E_INVALID;
- * FLUID_E_ARENA_TOO_SMALL (workspace). */
+ * shared by few workgroups, and slower than with a kv_max near their length.
+ * workspace: 256-byte aligned device memory of at least the bytes
+ * fluid_kv_attention_workspace returns for the same arguments (0: NULL will do),
+ * for this call alone while it runs.  Arithmetic: products on the f16 matrix
+ * cores with fp32 sums, softmax in fp32.  bf16: a query's channels below 2^-14 of
+ * its largest are rounded to 2^-25 of that, and a weight to f16 (11 bits) for its
+ * product with the value.  fp32: queries and weights are two f16 parts each,
+ * within 2^-22 of themselves and queries within 2^-25 of the row's largest: up to
+ * four times an fp32 rounding.  Errors: FLUID_E_INVALID; FLUID_E_ARENA_TOO_SMALL
+ * (workspace). */
 fluid_status fluid_kv_attention_workspace(const fluid_kv_cache* cache, const fluid_attention_opts* opts,
                                           int32_t kv_max, const fluid_tokens* qd, uint64_t* bytes);
 fluid_status fluid_kv_attention(const fluid_kv_cache* cache, const void* pool, const int32_t* pages,
