@@ -1,8 +1,9 @@
 /*
  * fluid_attention.h -- token-by-token generation next to the planned graphs
  * of fluid.h: a paged key/value cache held in 4 bits, the attention that
- * reads it, and attention over ordinary keys and values with a sliding window
- * and a few first tokens that stay visible.
+ * reads it, attention over ordinary keys and values with a sliding window
+ * and a few first tokens that stay visible, linear attention with a decay, and
+ * rotary positions at a sequence's own place.
  *
  * Conventions are those of fluid.h: every call returns a fluid_status and
  * nothing throws across the ABI (fluid_last_error() has the cause), arguments
@@ -154,6 +155,78 @@ fluid_status fluid_attention(const fluid_attention_opts* opts, const fluid_token
                              const fluid_tokens* kd, const void* k, const fluid_tokens* vd, const void* v,
                              const int32_t* q_len, const int32_t* kv_len, const fluid_tokens* od, void* out,
                              void* workspace, uint64_t workspace_bytes, void* hip_stream);
+
+/* Rotary positions: pairs of a head's first `dim` channels turn by the angle
+ * p * theta_i at position p, i < dim / 2; the channels behind them stay.
+ *     pair i: channels i and i + dim / 2, or 2 i and 2 i + 1 if interleaved
+ *     theta_i = base^(-2 i / dim)
+ * and for contexts `factor` times as long
+ *     LINEAR  theta_i / factor
+ *     BASE    with base * factor^(dim / (dim - 2)); dim at least 4
+ *     RAMP    theta_i where it makes r = length * theta_i / (2 pi) >= high turns
+ *             over `length` tokens, theta_i / factor where r <= low, and between
+ *             them their mix with the share (r - low) / (high - low) of theta_i
+ * Turned channels are multiplied by amplitude.  (x, y) becomes
+ * amplitude * (x cos - y sin, y cos + x sin). */
+typedef enum {
+  FLUID_ROTARY_NONE = 0, FLUID_ROTARY_LINEAR = 1, FLUID_ROTARY_BASE = 2, FLUID_ROTARY_RAMP = 3
+} fluid_rotary_scaling;
+typedef struct {
+  int32_t dim;         /* even, 2 .. 1024 */
+  int32_t interleaved; /* 0 or 1 */
+  int32_t scaling;     /* fluid_rotary_scaling; NONE uses none of the fields behind base */
+  float amplitude;     /* finite */
+  double base;         /* >= 1 */
+  double factor;       /* positive */
+  double length, low, high; /* RAMP only: length > 0, low < high */
+} fluid_rotary;
+
+/* The turns that each pair makes from a position to the next, theta_i / (2 pi)
+ * in units of 2^-64 modulo whole turns, into turns[dim / 2] in host memory; the
+ * caller copies them to the device once.  Multiplied by any int32 position modulo
+ * 2^64 they leave the angle within 2^-33 of a turn.  Needs no GPU.  Errors:
+ * FLUID_E_INVALID. */
+fluid_status fluid_rotary_turns(const fluid_rotary* r, uint64_t* turns);
+
+/* q [batch, T, heads, head_dim] and k [batch, T, kv_heads, head_dim] turned into
+ * qo and ko of their shapes, one dtype for all; kd NULL: no k.  Any head_dim
+ * from dim to 1024.  Row i of sequence b is at position positions[b *
+ * position_stride + i], or start[b] + i (start NULL: i); not both; negative ones
+ * too.  Rows from count[b] on (NULL: T; clamped to [0, T]) are left as they are.
+ * inverse 1 turns back, which is the gradient as well.  An output may be its own
+ * input, with the same strides; else they must not overlap.  turns: device
+ * memory, 8-byte aligned, what fluid_rotary_turns gave for r.  fp32 arithmetic,
+ * rounded once.  Errors: FLUID_E_INVALID. */
+fluid_status fluid_rotate(const fluid_rotary* r, const uint64_t* turns, const int32_t* start,
+                          const int32_t* positions, int64_t position_stride, const int32_t* count, int32_t inverse,
+                          const fluid_tokens* qd, const void* q, const fluid_tokens* qod, void* qo,
+                          const fluid_tokens* kd, const void* k, const fluid_tokens* kod, void* ko, void* hip_stream);
+
+/* Linear attention with a decay.  For every sequence and kv head, from the
+ * state S [head_dim of keys][head_dim of values] on, token after token
+ *     S = exp(g_t) S + k_t v_t^T        o_t = scale * S^T q_t
+ * with q, out [batch, T, heads, head_dim], k, v [batch, T, kv_heads, head_dim] of
+ * one dtype, heads a multiple of kv_heads (query head h reads the state of kv
+ * head h / (heads / kv_heads)).  decay: g, fp32, at element b stride[0] + t
+ * stride[1] + h stride[2] (0 repeats: {0, 0, 1} is one decay a head); meant to be
+ * at most 0, and taken for -200 where it is below, which leaves nothing of S.
+ * state, state_out: fp32 [batch, kv_heads, head_dim, head_dim], dense, 16-byte
+ * aligned; the same or apart; state NULL starts from zeros, state_out NULL keeps
+ * none.  count[b] (NULL: T; clamped to [0, T]) tokens of sequence b are there;
+ * rows of out behind them are left as they are, and rows of q, k, v and g behind
+ * them are not used.  workspace: as fluid_attention.
+ * Arithmetic: fp32 sums and states.  fp32: fp32 products.  bf16: products on the
+ * bf16 matrix cores; the state's own are exact to 2^-23, out's factors (q k with
+ * its decay, and the state) are two bf16 parts each, 2^-16.  What is not finite in
+ * q makes its row not finite, in k and v its and all later rows' and the state,
+ * where NaN may stand for an infinity; rows before it stay.  Errors:
+ * FLUID_E_INVALID; FLUID_E_ARENA_TOO_SMALL (workspace). */
+fluid_status fluid_linear_attention_workspace(const fluid_tokens* qd, const fluid_tokens* kd, uint64_t* bytes);
+fluid_status fluid_linear_attention(float scale, const fluid_tokens* qd, const void* q, const fluid_tokens* kd,
+                                    const void* k, const fluid_tokens* vd, const void* v, const float* decay,
+                                    const int64_t decay_stride[3], const float* state, const int32_t* count,
+                                    const fluid_tokens* od, void* out, float* state_out, void* workspace,
+                                    uint64_t workspace_bytes, void* hip_stream);
 
 #ifdef __cplusplus
 }

@@ -1,13 +1,15 @@
 """Token-by-token generation beside the planned graphs: a paged key/value
-cache held in 4 bits, attention over it, and attention with a sliding window
-and a few first tokens that stay visible (ctypes binding of
-include/fluid_attention.h).
+cache held in 4 bits, attention over it, attention with a sliding window
+and a few first tokens that stay visible, linear attention with a decay, and
+rotary positions (ctypes binding of include/fluid_attention.h).
 
     kv_write(pool, pages, k, v, start, count)   quantise new tokens into the cache
     kv_read(pool, pages, start, k, v, count)    its values as ordinary tensors
     kv_attention(pool, pages, q, kv_len, ...)   queries over the cache
     attention(q, k, v, ...)                     queries over ordinary keys and values
     KvCache                                     pool, page table and lengths of a batch
+    linear_attention(q, k, v, decay, ...)       attention with a state instead of a cache
+    Rotary, rotary(turns, q, k, ...)            queries and keys turned by their positions
 
 Tensors of tokens are torch tensors [batch, tokens, heads, head_dim] in fp32
 or bf16 on the GPU, with any strides and contiguous channels; lengths, starts
@@ -45,6 +47,11 @@ class Opts(C.Structure):
     _fields_ = [("scale", C.c_float), ("causal", _I32), ("window", _I32), ("sinks", _I32)]
 
 
+class RotaryDesc(C.Structure):
+    _fields_ = [("dim", _I32), ("interleaved", _I32), ("scaling", _I32), ("amplitude", C.c_float)] + [
+        (name, C.c_double) for name in ("base", "factor", "length", "low", "high")]
+
+
 _PROTOS = {
     "fluid_kv_pool_bytes": [_VP, _VP],
     "fluid_kv_write": [_VP] * 10,
@@ -53,6 +60,10 @@ _PROTOS = {
     "fluid_kv_attention": [_VP, _VP, _VP, _VP, _I32, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _U64, _VP],
     "fluid_attention_workspace": [_VP] * 4,
     "fluid_attention": [_VP] * 12 + [_U64, _VP],
+    "fluid_rotary_turns": [_VP] * 2,
+    "fluid_rotate": [_VP] * 4 + [C.c_int64, _VP, _I32] + [_VP] * 9,
+    "fluid_linear_attention_workspace": [_VP] * 3,
+    "fluid_linear_attention": [C.c_float] + [_VP] * 14 + [_U64, _VP],
 }
 SYMBOLS = tuple(_PROTOS)
 
@@ -389,6 +400,172 @@ def attention(q, k, v, q_len=None, kv_len=None, scale=None, causal=True, window=
         _record(stream, dev, q, k, v, q_len, kv_len, out, workspace)
     del keep
     return out
+
+
+def _linear_call(q, k, v, decay, state, count, out, state_out):
+    torch = _torch()
+    dev = _device_of(q, "q")
+    qd, kd, vd = _describe(q, "q", dev), _describe(k, "k", dev), _describe(v, "v", dev)
+    od = _describe(out, "out", dev)
+    B, T, Hk, D = k.shape
+    if decay.dtype != torch.float32 or tuple(decay.shape) not in ((Hk,), (B, T, Hk)) or decay.get_device() != dev:
+        _refuse(f"decay: fp32 [{Hk}] or [{B}, {T}, {Hk}] on GPU {dev} is needed")
+    stride = (C.c_int64 * 3)(*((0, 0) + decay.stride() if decay.dim() == 1 else decay.stride()))
+    for name, t in (("state", state), ("state_out", state_out)):
+        if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != (B, Hk, D, D) or not t.is_contiguous()
+                              or t.get_device() != dev):
+            _refuse(f"{name}: contiguous fp32 [{B}, {Hk}, {D}, {D}] on GPU {dev} is needed")
+    _check_ints(count, "count", B, dev)
+    need = _U64()
+    fluid._check(_lib().fluid_linear_attention_workspace(_addr(qd), _addr(kd), C.byref(need)))
+    return (_lib(), dev, _addr(qd), _addr(kd), _addr(vd), _addr(od), _addr(stride), need.value, (qd, kd, vd, od, stride))
+
+
+def linear_attention(q, k, v, decay, state=None, count=None, scale=None, out=None, state_out=None, workspace=None,
+                     stream=None):
+    """Attention whose memory is a state S [head_dim, head_dim] of every kv
+    head: token after token S = exp(decay) S + k v^T, out = scale S^T q.
+
+    q [batch, T, heads, head_dim], k and v [batch, T, kv_heads, head_dim] (heads
+    a multiple of kv_heads) of one dtype; decay: its logarithm in fp32, at most 0,
+    [kv_heads] or one a token [batch, T, kv_heads].  state: fp32 [batch, kv_heads,
+    head_dim, head_dim] to start from (None: zeros); state_out: where to leave the
+    last one, which may be ``state`` (allocated by default).  count[b] (None: T)
+    tokens of sequence b are there; out's rows behind them are left as they are.
+    scale: 1 / sqrt(head_dim) by default.  A prompt and the single tokens behind
+    it are calls that hand the state on.  Returns (out, state_out)."""
+    if out is None:
+        out = _zeros(q, stream)
+    _check_grad(q, k, v, decay, out, *(t for t in (state, state_out) if t is not None))
+    if state_out is None:
+        state_out = _new_state(k, stream)
+    key = (fluid._lib, q.dtype, q.shape, q.stride(), q.get_device(), k.dtype, k.shape, k.stride(), k.get_device(),
+           v.dtype, v.shape, v.stride(), v.get_device(), out.dtype, out.shape, out.stride(), out.get_device(),
+           _form(decay), None if state is None else _form(state), _form(state_out),
+           None if count is None else _form(count), "linear")
+    made = _calls.get(key)
+    if made is None:
+        made = _keep(key, _linear_call(q, k, v, decay, state, count, out, state_out))
+    lib, dev, qd, kd, vd, od, stride, need, _ = made
+    keep, ws, ws_bytes = _workspace(need, workspace, dev, stream) if need else (None, None, 0)
+    _launch(lib.fluid_linear_attention, dev,
+            q.shape[3] ** -0.5 if scale is None else scale, qd, q.data_ptr(), kd, k.data_ptr(), vd, v.data_ptr(),
+            decay.data_ptr(), stride, None if state is None else state.data_ptr(),
+            None if count is None else count.data_ptr(), od, out.data_ptr(), state_out.data_ptr(), ws, ws_bytes,
+            _raw_stream(dev) if stream is None else _stream(stream, dev))
+    if stream is not None:
+        _record(stream, dev, q, k, v, decay, state, count, out, state_out, workspace)
+    del keep
+    return out, state_out
+
+
+def linear_attention_workspace(q, k):
+    """Bytes of workspace that ``linear_attention`` needs for these tensors."""
+    dev = _device_of(q, "q")
+    qd, kd, need = _describe(q, "q", dev), _describe(k, "k", dev), _U64()
+    fluid._check(_lib().fluid_linear_attention_workspace(_addr(qd), _addr(kd), C.byref(need)))
+    return need.value
+
+
+def _new_state(k, stream):
+    """A state for k's sequences and heads, allocated on the call's stream."""
+    torch = _torch()
+    if k.dim() != 4:
+        _refuse(f"k: a tensor [batch, tokens, heads, head_dim] is needed, got {k.dim()} dimensions")
+    shape = (k.shape[0], k.shape[2], k.shape[3], k.shape[3])
+    if stream is None or not k.is_cuda:
+        return torch.empty(shape, dtype=torch.float32, device=k.device)
+    with torch.cuda.stream(_as_stream(stream, k.device)):
+        return torch.empty(shape, dtype=torch.float32, device=k.device)
+
+
+SCALINGS = {"none": 0, "linear": 1, "base": 2, "ramp": 3}
+
+
+class Rotary:
+    """How positions turn a head's first ``dim`` channels: frequencies
+    base^(-2 i / dim) of pairs (i, i + dim / 2), or (2 i, 2 i + 1) if
+    ``interleaved``, for contexts ``factor`` times as long by one of
+    ``scaling``:
+
+        "linear"  all frequencies divided by factor
+        "base"    base * factor^(dim / (dim - 2))
+        "ramp"    frequencies that make ``high`` turns or more over ``length``
+                  tokens stay, those of ``low`` or fewer are divided, the others
+                  mixed in proportion
+
+    Turned channels are multiplied by ``amplitude``.  ``turns`` holds the pairs'
+    turns a token on the GPU, made once."""
+
+    def __init__(self, dim, base=10000.0, interleaved=False, scaling="none", factor=1.0, length=0.0, low=1.0, high=32.0,
+                 amplitude=1.0, device="cuda"):
+        torch = _torch()
+        if scaling not in SCALINGS:
+            _refuse(f"scaling: one of {', '.join(SCALINGS)} is needed, got {scaling!r}")
+        self.desc = RotaryDesc(dim, 1 if interleaved else 0, SCALINGS[scaling], amplitude, base, factor, length, low, high)
+        if not 2 <= dim <= 1024:
+            _refuse(f"dim: {dim} does not lie in 2 .. 1024")
+        turns = torch.empty(dim // 2, dtype=torch.int64)
+        fluid._check(_lib().fluid_rotary_turns(_addr(self.desc), turns.data_ptr()))
+        self.dim = dim
+        self.turns = turns.to(device)
+
+
+def _rotary_call(turns, q, k, start, positions, count, q_out, k_out):
+    torch = _torch()
+    dev = _device_of(q, "q")
+    if not isinstance(turns, Rotary):
+        _refuse("turns: a Rotary is needed")
+    if turns.turns.get_device() != dev:
+        _refuse(f"turns: on {turns.turns.device}, not on GPU {dev}")
+    qd, qod = _describe(q, "q", dev), _describe(q_out, "q_out", dev)
+    kd = kod = None
+    if k is not None:
+        kd, kod = _describe(k, "k", dev), _describe(k_out, "k_out", dev)
+    elif k_out is not None:
+        _refuse("k_out: there is no k")
+    B, T = q.shape[:2]
+    _check_ints(start, "start", B, dev)
+    _check_ints(count, "count", B, dev)
+    stride = 0
+    if positions is not None:
+        if (positions.dtype != torch.int32 or tuple(positions.shape) != (B, T) or positions.get_device() != dev
+                or (T > 1 and positions.stride(1) != 1)):
+            _refuse(f"positions: int32 [{B}, {T}] with contiguous rows on GPU {dev} is needed")
+        stride = positions.stride(0)
+    refs = [None if d is None else _addr(d) for d in (qd, qod, kd, kod)]
+    return (_lib(), dev, *refs, stride, (qd, qod, kd, kod))
+
+
+def rotary(turns, q, k=None, start=None, positions=None, count=None, inverse=False, q_out=None, k_out=None, stream=None):
+    """q [batch, T, heads, head_dim] and k [batch, T, kv_heads, head_dim] (None:
+    q alone) turned by their positions as ``turns``, a Rotary, says.
+
+    Row i of sequence b is at position start[b] + i (None: i), or at positions[b,
+    i].  Rows from count[b] on (None: T) are left as they are.  inverse: turned
+    back.  q_out, k_out: where to write, which may be q and k themselves
+    (allocated as zeros by default).  Returns (q_out, k_out), or q_out without a
+    k."""
+    if q_out is None:
+        q_out = _zeros(q, stream)
+    if k is not None and k_out is None:
+        k_out = _zeros(k, stream)
+    _check_grad(q, q_out, *(t for t in (k, k_out) if t is not None))
+    key = (fluid._lib, q.dtype, q.shape, q.stride(), q.get_device(), _form(k), q_out.dtype, q_out.shape, q_out.stride(),
+           q_out.get_device(), _form(k_out), _form(start), _form(positions), _form(count),
+           type(turns) is Rotary and turns.turns.get_device(), "rotary")
+    made = _calls.get(key)
+    if made is None:
+        made = _keep(key, _rotary_call(turns, q, k, start, positions, count, q_out, k_out))
+    lib, dev, qd, qod, kd, kod, stride, _ = made
+    _launch(lib.fluid_rotate, dev, C.addressof(turns.desc), turns.turns.data_ptr(),
+            None if start is None else start.data_ptr(), None if positions is None else positions.data_ptr(), stride,
+            None if count is None else count.data_ptr(), 1 if inverse else 0, qd, q.data_ptr(), qod, q_out.data_ptr(),
+            kd, None if k is None else k.data_ptr(), kod, None if k_out is None else k_out.data_ptr(),
+            _raw_stream(dev) if stream is None else _stream(stream, dev))
+    if stream is not None:
+        _record(stream, dev, q, k, start, positions, count, q_out, k_out, turns.turns)
+    return q_out if k is None else (q_out, k_out)
 
 
 class KvCache:

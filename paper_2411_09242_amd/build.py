@@ -74,11 +74,12 @@ def build(host_only=False, jobs=None, force=False):
         shutil.rmtree(BUILD)
     os.makedirs(LIBDIR, exist_ok=True)
     host_srcs = sorted(glob.glob(os.path.join(CSRC, "host", "*.cpp")))
-    host_srcs += sorted(glob.glob(os.path.join(CSRC, "attn", "*.cpp")))
+    host_srcs += sorted(glob.glob(os.path.join(CSRC, "attn", "*.cpp")) + glob.glob(os.path.join(CSRC, "w4", "*.cpp")))
     stubs = ("host_stubs.cpp", "backend_host.cpp")
     core = [s for s in host_srcs if not s.endswith(stubs)]
     stub = [s for s in host_srcs if s.endswith(stubs)]
-    hip_srcs = sorted(glob.glob(os.path.join(CSRC, "gpu", "*.hip")) + glob.glob(os.path.join(CSRC, "attn", "*.hip")))
+    hip_srcs = sorted(glob.glob(os.path.join(CSRC, "gpu", "*.hip")) + glob.glob(os.path.join(CSRC, "attn", "*.hip"))
+                      + glob.glob(os.path.join(CSRC, "w4", "*.hip")))
     jobs_list = [(s, _obj(s, "host"), ["g++"] + CXXFLAGS) for s in core + stub]
     if not host_only:
         jobs_list += [(s, _obj(s, "gpu"), [HIPCC] + HIPFLAGS) for s in hip_srcs]

@@ -43,7 +43,8 @@ def _compile(src):
 def build():
     os.makedirs(BUILD, exist_ok=True)
     os.makedirs(LIBDIR, exist_ok=True)
-    srcs = sorted(glob.glob(os.path.join(CSRC, "host", "*.cpp")) + glob.glob(os.path.join(CSRC, "attn", "*.cpp")))
+    srcs = sorted(glob.glob(os.path.join(CSRC, "host", "*.cpp")) + glob.glob(os.path.join(CSRC, "attn", "*.cpp"))
+                  + glob.glob(os.path.join(CSRC, "w4", "*.cpp")))
     with cf.ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 4)) as ex:
         objs = list(ex.map(_compile, srcs))
     lib = os.path.join(LIBDIR, "libfluid_host.so")

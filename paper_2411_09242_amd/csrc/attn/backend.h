@@ -9,5 +9,7 @@ namespace fluid {
 void run_kv_io(const KvIoParams& p, int dtype, int head_dim, bool write, void* stream);
 void run_kv_attention(const AttnParams& p, int dtype, int head_dim, void* stream);
 void run_attention(const AttnParams& p, int dtype, int head_dim, void* stream);
+void run_rotate(const RotaryParams& p, int dtype, void* stream);
+void run_linear_attention(const LinearParams& p, int dtype, int head_dim, void* stream);
 
 }  // namespace fluid

@@ -20,5 +20,11 @@ void run_kv_attention(const AttnParams& p, int dtype, int head_dim, void* stream
 void run_attention(const AttnParams& p, int dtype, int head_dim, void* stream) {
   check(launch_attention(p, dtype, head_dim, (hipStream_t)stream), "fluid_attention");
 }
+void run_rotate(const RotaryParams& p, int dtype, void* stream) {
+  check(launch_rotate(p, dtype, (hipStream_t)stream), "fluid_rotate");
+}
+void run_linear_attention(const LinearParams& p, int dtype, int head_dim, void* stream) {
+  check(launch_linear_attention(p, dtype, head_dim, (hipStream_t)stream), "fluid_linear_attention");
+}
 
 }  // namespace fluid

@@ -13,5 +13,7 @@ namespace {
 void run_kv_io(const KvIoParams&, int, int, bool write, void*) { unsupported(write ? "fluid_kv_write" : "fluid_kv_read"); }
 void run_kv_attention(const AttnParams&, int, int, void*) { unsupported("fluid_kv_attention"); }
 void run_attention(const AttnParams&, int, int, void*) { unsupported("fluid_attention"); }
+void run_rotate(const RotaryParams&, int, void*) { unsupported("fluid_rotate"); }
+void run_linear_attention(const LinearParams&, int, int, void*) { unsupported("fluid_linear_attention"); }
 
 }  // namespace fluid

@@ -59,6 +59,41 @@ struct AttnParams {
   float* ws;       // splits > 1: [item][split] of row_tile maxima, sums and rows of partial sums
 };
 
+// Queries and keys (the second ones, if any) turned by their positions.
+struct RotaryParams {
+  TokensArg x[2], y[2];
+  int32_t heads[2];
+  const uint64_t* turns;
+  const int32_t* start;
+  const int32_t* positions;
+  int64_t position_stride;
+  const int32_t* count;
+  int32_t batch, tokens, head_dim, dim;
+  int32_t interleaved, inverse, tail;  // tail: channels behind dim are copied
+  float amplitude;
+  int32_t vec;           // 16 bytes at a time
+  int32_t units, pairs;  // of a head: in all, of turned ones
+  int32_t head_threads;  // that share a token's heads
+  uint32_t items;        // threads
+  FastDiv div_units, div_heads, div_tokens;
+};
+
+// Linear attention: a state per kv head.
+struct LinearParams {
+  TokensArg q, k, v, o;
+  const float* decay;
+  int64_t gb, gt, gh;
+  const float* state;  // may be state_out
+  float* state_out;
+  const int32_t* count;
+  int32_t batch, tokens, kv_heads, group;
+  float scale;
+  FastDiv div_heads;
+  int32_t segments;  // runs of tokens that workgroups of their own take
+  int32_t run;       // tokens of a run
+  float* ws;
+};
+
 // tokens of a step over the 4-bit cache, and over bf16 and fp32 keys and values
 constexpr int kKvTile = 32, kBf16Tile = 64, kF32Tile = 32;
 

@@ -1,0 +1,124 @@
+// Entry points of fluid_w4.h: argument checks and launch sizes.
+#include "fluid_w4.h"
+
+#include <cstdint>
+
+#include "../host/handles.h"
+#include "../host/kparams.h"
+#include "w4_backend.h"
+
+namespace fluid {
+
+namespace {
+
+W4Params check_shape(const fluid_w4* w) {
+  require(w != nullptr, "w: NULL");
+  require(w->rows >= 1 && w->cols >= 1, "w: rows and cols must be at least 1");
+  require(w->group == 32 || w->group == 64 || w->group == 128, "w: group must be 32, 64 or 128");
+  require(w->rows <= 1 << 30 && w->cols <= 1 << 30, "w: more than 2^30 rows or cols");
+  W4Params p{};
+  p.n = w->rows;
+  p.k = w->cols;
+  p.group = w->group;
+  p.tiles = (w->rows + 15) / 16;
+  p.blocks = (w->cols + 127) / 128;
+  return p;
+}
+int64_t word_bytes(const W4Params& p) { return int64_t(p.tiles) * p.blocks * 1024; }
+uint64_t bytes_of(const W4Params& p) {
+  return uint64_t(word_bytes(p)) + uint64_t(p.tiles) * p.blocks * 64 * (128 / p.group);
+}
+W4Arg held(const W4Params& p, const void* packed, const char* name) {
+  require(packed != nullptr, name, ": NULL data");
+  require((uintptr_t)packed % 16 == 0, name, ": must be 16-byte aligned");
+  return {(const uint8_t*)packed, (const uint8_t*)packed + word_bytes(p)};
+}
+
+// Stride of a matrix's rows, in elements.
+int64_t check_matrix(const fluid_matrix* d, const void* data, int32_t cols, const char* name) {
+  require(d != nullptr, name, ": NULL description");
+  require(data != nullptr, name, ": NULL data");
+  require(d->dtype == FLUID_F32 || d->dtype == FLUID_BF16, name, ": dtype must be f32 or bf16");
+  require((uintptr_t)data % dtype_bytes(d->dtype) == 0, name, ": misaligned for its type");
+  require(d->rows >= 1 && d->cols >= 1, name, ": rows and cols must be at least 1");
+  require(d->cols == cols, name, ": cols do not fit the matrix");
+  if (d->rows == 1) return 0;
+  require(d->stride >= 0 && d->stride <= (int64_t(1) << 40), name, ": stride must lie in 0 .. 2^40");
+  return d->stride;
+}
+void check_apart(const fluid_matrix* d, const char* name) {
+  require(d->rows == 1 || d->stride >= d->cols, name, ": an output's stride must be at least its cols");
+}
+
+}  // namespace
+
+}  // namespace fluid
+
+using namespace fluid;
+
+extern "C" {
+
+fluid_status fluid_w4_bytes(const fluid_w4* w, uint64_t* bytes) {
+  return call_guarded([&] {
+    const W4Params p = check_shape(w);
+    require(bytes != nullptr, "bytes: NULL");
+    *bytes = bytes_of(p);
+  });
+}
+
+fluid_status fluid_w4_pack(const fluid_w4* w, const fluid_matrix* md, const void* m, void* packed, void* hip_stream) {
+  return call_guarded([&] {
+    W4Params p = check_shape(w);
+    p.w = held(p, packed, "packed");
+    p.xs = check_matrix(md, m, w->cols, "m");
+    require(md->rows == w->rows, "m: rows do not fit the matrix");
+    require(int64_t(p.tiles) * p.blocks <= int64_t(1) << 23, "w: too large for one launch");
+    p.x = m;
+    run_w4_pack(p, md->dtype, hip_stream);
+  });
+}
+
+fluid_status fluid_w4_read(const fluid_w4* w, const void* packed, const fluid_matrix* md, void* m, void* hip_stream) {
+  return call_guarded([&] {
+    W4Params p = check_shape(w);
+    p.w = held(p, packed, "packed");
+    p.os = check_matrix(md, m, w->cols, "m");
+    require(md->rows == w->rows, "m: rows do not fit the matrix");
+    check_apart(md, "m");
+    require(int64_t(p.tiles) * p.blocks <= int64_t(1) << 23, "w: too large for one launch");
+    p.out = m;
+    run_w4_read(p, md->dtype, hip_stream);
+  });
+}
+
+fluid_status fluid_w4_matmul(const fluid_w4* w, const void* packed, const void* gate, const fluid_matrix* xd,
+                             const void* x, const fluid_matrix* ad, const void* add, const fluid_matrix* od, void* out,
+                             void* hip_stream) {
+  return call_guarded([&] {
+    W4Params p = check_shape(w);
+    p.w = held(p, packed, "packed");
+    if (gate != nullptr) p.gate = held(p, gate, "gate");
+    p.xs = check_matrix(xd, x, w->cols, "x");
+    p.os = check_matrix(od, out, w->rows, "out");
+    require(od->dtype == xd->dtype && od->rows == xd->rows, "out must have x's dtype and rows");
+    check_apart(od, "out");
+    if (add != nullptr) {
+      p.as = check_matrix(ad, add, w->rows, "add");
+      require(ad->dtype == xd->dtype && ad->rows == xd->rows, "add must have x's dtype and rows");
+      require(add != out || p.as == p.os, "out: where it is add it must have its stride");
+    }
+    require(out != x, "out must not be x");
+    require(xd->rows <= 64 * 65535, "x: too many rows for one launch");
+    require(int64_t(p.tiles) * 1024 < int64_t(1) << 32, "w: too large for one launch");
+    p.x = x;
+    p.add = add;
+    p.out = out;
+    p.m = xd->rows;
+    p.vec = (uintptr_t)x % 16 == 0 && (p.xs * dtype_bytes(xd->dtype)) % 16 == 0;
+    // wavefronts with blocks of their own; more rows take more registers
+    p.waves = p.blocks >= 16 && p.m <= 16 ? 16 : p.blocks >= 8 ? 8 : 4;
+    run_w4_matmul(p, xd->dtype, hip_stream);
+  });
+}
+
+}  // extern "C"

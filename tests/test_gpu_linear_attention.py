@@ -1,0 +1,267 @@
+"""Linear attention on the GPU against plain NumPy in 64 bits, token after token
+(oracle/decoder_layers.py).
+
+Tolerance.  With u = 2^-24, T tokens and M the sums of sizes that the oracle
+returns beside out and state: a term of the state passes T products with a decay,
+each decay within 2 u of itself, and T additions: 3 T u M with 16 u for its own
+product and the exponentials' arguments.  out adds D terms of it and the scale:
+(3 T + D + 16) u M.  bf16 tensors: the factors of out's products are two bf16 parts
+(each cut off or rounded: 2^-15 in all), in q k with its decay and in the state,
+and the output is rounded by 2^-8 of itself.  The state's products: v with its
+decay in three parts, 2^-23."""
+import numpy as np
+import pytest
+
+from oracle import decoder_layers as O
+
+torch = pytest.importorskip("torch")
+from paper_2411_09242_amd import attention as A  # noqa: E402
+from paper_2411_09242_amd import fluid as F  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+U = 2.0 ** -24
+
+
+@pytest.fixture(scope="module", autouse=True)
+def gpu_lib():
+    F.load()
+    yield
+
+
+def ints(v):
+    return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+def rand(seed, *shape, dtype="f32", scale=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(*shape, generator=g) * scale).to(DT[dtype]).cuda()
+
+
+def host(t):
+    return t.detach().cpu().to(torch.float64).numpy()
+
+
+def decays(seed, B, T, Hk, per_token):
+    """Memories of a few to some thousand tokens; with tokens' own decays some
+    forget everything."""
+    if not per_token:
+        return torch.log1p(-torch.exp2(-2.0 - 8.0 * torch.rand(Hk, generator=torch.Generator().manual_seed(seed)))).cuda()
+    g = -torch.nn.functional.softplus(rand(seed, B, T, Hk) * 2 - 3)
+    g[rand(seed + 1, B, T, Hk) > 2.5] = float("-inf")
+    return g
+
+
+def laid_out(t, how):
+    """The same values in other strides."""
+    B, T, H, D = t.shape
+    if how == "heads_first":
+        return t.transpose(1, 2).contiguous().transpose(1, 2)
+    pad = {"padded": 16, "odd": 3}[how]
+    buf = torch.full((B, T, H, D + pad), 7.0, dtype=t.dtype, device=t.device)
+    off = 1 if how == "odd" else 0
+    buf[..., off:off + D] = t
+    return buf[..., off:off + D]
+
+
+def check(got, q, k, v, g, state, counts, scale, dtype, heads=None, before=9.0):
+    """(out, state_out) of the (sequence, kv head) pairs in `heads`, or of all."""
+    out, last = host(got[0]), host(got[1])
+    B, T, H, D = q.shape
+    Hk = k.shape[2]
+    q, k, v = host(q), host(k), host(v)
+    g = host(g) if g.dim() == 3 else np.broadcast_to(host(g), (B, T, Hk))
+    state = np.zeros((B, Hk, D, D)) if state is None else host(state)
+    group = H // Hk
+    for b, h in heads or [(b, h) for b in range(B) for h in range(Hk)]:
+        n = counts[b]
+        rows = slice(h * group, (h + 1) * group)
+        o, S, size, M = O.linear_attention(q[b, :n, rows], k[b, :n, h], v[b, :n, h], g[b, :n, h], state[b, h], scale)
+        part = 2.0 ** -15 if dtype == "bf16" else 0.0
+        tol = ((3 * n + D + 16) * U + 2 * part) * size + (2.0 ** -8 * np.abs(o) if dtype == "bf16" else 0.0)
+        err = np.abs(out[b, :n, rows] - o)
+        assert (err <= tol).all(), ("out", b, h, (err / np.maximum(tol, 1e-30)).max())
+        tol = (3 * n + 16) * U * M + (2.0 ** -22 * M if dtype == "bf16" else 0.0)
+        err = np.abs(last[b, h] - S)
+        assert (err <= tol).all(), ("state", b, h, (err / np.maximum(tol, 1e-30)).max())
+        assert (out[b, n:, rows] == before).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [32, 64, 128])
+@pytest.mark.parametrize("T", [1, 2, 5, 16, 17, 31, 64, 65, 130])
+@pytest.mark.parametrize("per_token", [False, True])
+def test_rows_and_states(dtype, D, T, per_token):
+    B, H, Hk = 3, 4, 2
+    q, k, v = rand(1, B, T, H, D, dtype=dtype), rand(2, B, T, Hk, D, dtype=dtype), rand(3, B, T, Hk, D, dtype=dtype)
+    g, state = decays(4, B, T, Hk, per_token), rand(5, B, Hk, D, D, scale=3.0)
+    counts = [T, 0, max(1, T - T // 3)]
+    out = torch.full_like(q, 9.0)
+    got = A.linear_attention(q, k, v, g, state=state, count=ints(counts), scale=0.3, out=out)
+    assert got[0] is out
+    check(got, q, k, v, g, state, counts, 0.3, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("how", ["heads_first", "padded", "odd"])
+@pytest.mark.parametrize("T", [3, 100])
+def test_strides(dtype, how, T):
+    B, H, Hk, D = 2, 6, 3, 64
+    q, k, v = (laid_out(rand(i, B, T, h, D, dtype=dtype), how) for i, h in ((1, H), (2, Hk), (3, Hk)))
+    out = laid_out(torch.full((B, T, H, D), 9.0, dtype=DT[dtype], device="cuda"), how)
+    g = decays(4, B, T, Hk, True).transpose(1, 2).contiguous().transpose(1, 2)
+    got = A.linear_attention(q, k, v, g, scale=0.5, out=out)
+    check(got, q, k, v, g, None, [T] * B, 0.5, dtype)
+    if how != "heads_first":
+        assert (out._base[..., D + (1 if how == "odd" else 0):] == 7.0).all()
+
+
+@pytest.mark.parametrize("dtype, B, T, H, Hk, D", [("bf16", 1, 2048, 4, 4, 128), ("bf16", 2, 1500, 8, 2, 64),
+                                                   ("f32", 1, 1111, 4, 2, 128), ("f32", 2, 2000, 2, 2, 32),
+                                                   ("bf16", 40, 200, 16, 16, 128), ("f32", 33, 150, 16, 8, 64)])
+@pytest.mark.parametrize("per_token", [False, True])
+def test_long_prompts_and_many_heads(dtype, B, T, H, Hk, D, per_token):
+    q, k, v = rand(1, B, T, H, D, dtype=dtype), rand(2, B, T, Hk, D, dtype=dtype), rand(3, B, T, Hk, D, dtype=dtype)
+    g, state = decays(4, B, T, Hk, per_token), rand(5, B, Hk, D, D, scale=3.0)
+    counts = [T - (T // 3 if b % 2 else 0) for b in range(B)]
+    out = torch.full_like(q, 9.0)
+    got = A.linear_attention(q, k, v, g, state=state, count=ints(counts), scale=D ** -0.5, out=out)
+    check(got, q, k, v, g, state, counts, D ** -0.5, dtype, heads=[(0, 0), (B - 1, Hk - 1), (B // 2, Hk // 2), (0, Hk - 1)])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [1, 40, 700])
+def test_state_in_place_and_handed_on(dtype, T):
+    """A state may be its own successor; a prompt in two calls is one."""
+    B, H, D = 2, 3, 64
+    q, k, v = (rand(i, B, T, H, D, dtype=dtype) for i in (1, 2, 3))
+    g, state = decays(4, B, T, H, True), rand(5, B, H, D, D)
+    want = A.linear_attention(q, k, v, g, state=state, scale=0.1)
+    mine = state.clone()
+    out, last = A.linear_attention(q, k, v, g, state=mine, state_out=mine, scale=0.1)
+    assert last is mine and torch.equal(out, want[0]) and torch.equal(mine, want[1])
+    cut = T // 3
+    if cut:
+        part = lambda t, a, z: t[:, a:z]  # noqa: E731
+        first = A.linear_attention(*(part(t, 0, cut) for t in (q, k, v, g)), state=state, scale=0.1)
+        rest = A.linear_attention(*(part(t, cut, T) for t in (q, k, v, g)), state=first[1], scale=0.1)
+        both = torch.cat([first[0], rest[0]], 1)
+        check((both, rest[1]), q, k, v, g, state, [T] * B, 0.1, dtype)
+
+
+def test_one_by_one_is_as_all_at_once():
+    B, T, H, D = 1, 75, 2, 128
+    q, k, v = (rand(i, B, T, H, D, dtype="bf16") for i in (1, 2, 3))
+    g = decays(4, B, T, H, False)
+    state, rows = torch.zeros(B, H, D, D, device="cuda"), []
+    for t in range(T):
+        o, _ = A.linear_attention(*(x[:, t:t + 1] for x in (q, k, v)), g, state=state, state_out=state)
+        rows.append(o)
+    check((torch.cat(rows, 1), state), q, k, v, g, None, [T], D ** -0.5, "bf16")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_what_is_no_number_reaches_only_what_follows(dtype):
+    """Rows before it and other heads stay to the bit; padding is not used."""
+    B, T, H, D = 2, 150, 2, 64
+    q, k, v = (rand(i, B, T, H, D, dtype=dtype) for i in (1, 2, 3))
+    g, counts = decays(4, B, T, H, True).clamp(min=-5.0), ints([T, 100])
+    run = lambda: A.linear_attention(q, k, v, g, count=counts, scale=0.2)  # noqa: E731
+    clean = run()
+    for t in (q, k, v):
+        t[1, 100:] = float("nan")
+    g[1, 100:] = float("nan")
+    got = run()
+    assert torch.equal(got[0], clean[0]) and torch.equal(got[1], clean[1])
+    for t, name in ((q, "q"), (k, "k"), (v, "v")):
+        for value in (float("inf"), float("nan")):
+            old = t[0, 70, 0, 5].clone()
+            t[0, 70, 0, 5] = value
+            out, last = run()
+            t[0, 70, 0, 5] = old
+            assert torch.equal(out[0, :70], clean[0][0, :70]) and torch.equal(out[0, :, 1], clean[0][0, :, 1])
+            assert torch.equal(out[1], clean[0][1]) and torch.equal(last[1], clean[1][1])
+            assert torch.equal(last[0, 1], clean[1][0, 1])
+            bad = ~out[0, 70, 0].isfinite()
+            if name == "v":  # that channel of this and all later rows, and of the state
+                assert bad[5] and bad.sum() == 1 and not out[0, 70:, 0, 5].isfinite().any()
+                rest = [c for c in range(D) if c != 5]
+                assert torch.equal(out[0, :, 0][:, rest], clean[0][0, :, 0][:, rest])
+                assert not last[0, 0, :, 5].isfinite().any() and torch.equal(last[0, 0][:, rest], clean[1][0, 0][:, rest])
+            else:
+                assert bad.all()
+                if name == "q":
+                    assert torch.equal(out[0, 71:], clean[0][0, 71:]) and torch.equal(last, clean[1])
+
+
+def test_a_decay_of_nothing_forgets_everything():
+    B, T, H, D = 1, 90, 1, 32
+    q, k, v = (rand(i, B, T, H, D) for i in (1, 2, 3))
+    g = torch.zeros(B, T, H, device="cuda")
+    g[0, 50] = float("-inf")
+    g[0, 60] = -1e30
+    out, last = A.linear_attention(q, k, v, g, state=rand(5, B, H, D, D), scale=1.0)
+    fresh = A.linear_attention(q[:, 60:], k[:, 60:], v[:, 60:], g[:, 60:], scale=1.0)
+    check((out[:, 60:], last), q[:, 60:], k[:, 60:], v[:, 60:], torch.zeros_like(g[:, 60:]), None, [30], 1.0, "f32")
+    check(fresh, q[:, 60:], k[:, 60:], v[:, 60:], torch.zeros_like(g[:, 60:]), None, [30], 1.0, "f32")
+
+
+def test_a_graph_replays_and_moves_the_state_on():
+    B, H, D = 2, 4, 128
+    g = decays(1, B, 1, H, False)
+    q, k, v = (rand(i, B, 1, H, D, dtype="bf16") for i in (1, 2, 3))
+    out, state = torch.zeros_like(q), torch.zeros(B, H, D, D, device="cuda")
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        A.linear_attention(q, k, v, g, state=state, state_out=state, out=out)
+    torch.cuda.current_stream().wait_stream(s)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        A.linear_attention(q, k, v, g, state=state, state_out=state, out=out)
+    mirror = state.clone()
+    for i in range(5):
+        for j, t in enumerate((q, k, v)):
+            t.copy_(rand(10 * i + j, B, 1, H, D, dtype="bf16"))
+        graph.replay()
+        want, _ = A.linear_attention(q, k, v, g, state=mirror, state_out=mirror)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(state, mirror)
+
+
+def test_two_graphs_of_prompts_and_a_workspace():
+    """Captured calls allocate their workspace in the graph's own pool, or take
+    the caller's."""
+    B, T, H, D = 1, 1200, 2, 128
+    q, k, v = (rand(i, B, T, H, D, dtype="bf16") for i in (1, 2, 3))
+    g = decays(4, B, T, H, True)
+    need = A.linear_attention_workspace(q, k)
+    ws = torch.empty(max(need, 1), dtype=torch.uint8, device="cuda")
+    want = A.linear_attention(q, k, v, g)
+    outs = []
+    for w in (None, ws):
+        out, last = torch.zeros_like(q), torch.zeros(B, H, D, D, device="cuda")
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            A.linear_attention(q, k, v, g, out=out, state_out=last, workspace=w)
+        outs.append((graph, out, last))
+    for _ in range(3):
+        for graph, out, last in outs:
+            out.zero_(), last.zero_()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out, want[0]) and torch.equal(last, want[1])
+    if need:
+        with pytest.raises(F.FluidError, match="workspace"):
+            A.linear_attention(q, k, v, g, workspace=ws[:need - 256])
+
+
+def test_on_another_stream():
+    q, k, v = (rand(i, 2, 300, 4, 64, dtype="bf16") for i in (1, 2, 3))
+    g = decays(4, 2, 300, 4, True)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    got = A.linear_attention(q, k, v, g, stream=s)
+    torch.cuda.current_stream().wait_stream(s)
+    want = A.linear_attention(q, k, v, g)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
