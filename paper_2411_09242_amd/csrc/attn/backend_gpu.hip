@@ -24,7 +24,8 @@ void run_rotate(const RotaryParams& p, int dtype, void* stream) {
   check(launch_rotate(p, dtype, (hipStream_t)stream), "fluid_rotate");
 }
 void run_linear_attention(const LinearParams& p, int dtype, int head_dim, void* stream) {
-  check(launch_linear_attention(p, dtype, head_dim, (hipStream_t)stream), "fluid_linear_attention");
+  check((p.segments ? launch_linear_chunk : launch_linear_step)(p, dtype, head_dim, (hipStream_t)stream),
+        "fluid_linear_attention");
 }
 
 }  // namespace fluid

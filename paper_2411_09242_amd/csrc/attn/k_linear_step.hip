@@ -85,7 +85,7 @@ hipError_t launch_dim(const LinearParams& p, int D, hipStream_t s) {
 
 }  // namespace
 
-hipError_t launch_linear_attention(const LinearParams& p, int dtype, int head_dim, hipStream_t s) {
+hipError_t launch_linear_step(const LinearParams& p, int dtype, int head_dim, hipStream_t s) {
   return dtype == DT_BF16 ? launch_dim<uint16_t>(p, head_dim, s) : launch_dim<float>(p, head_dim, s);
 }
 

@@ -14,7 +14,8 @@ hipError_t launch_attention_f32(const AttnParams& p, int head_dim, hipStream_t s
 hipError_t launch_attention(const AttnParams& p, int dtype, int head_dim, hipStream_t s);
 
 hipError_t launch_rotate(const RotaryParams& p, int dtype, hipStream_t s);
-hipError_t launch_linear_attention(const LinearParams& p, int dtype, int head_dim, hipStream_t s);
+hipError_t launch_linear_step(const LinearParams& p, int dtype, int head_dim, hipStream_t s);
+hipError_t launch_linear_chunk(const LinearParams& p, int dtype, int head_dim, hipStream_t s);
 
 // Joins the shares of split rows (splits > 1), after either of the above.
 hipError_t launch_attention_join(const AttnParams& p, int dtype, int head_dim, hipStream_t s);

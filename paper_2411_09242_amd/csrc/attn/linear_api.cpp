@@ -18,14 +18,23 @@ LinearParams plan_linear(const fluid_tokens* qd, const fluid_tokens* kd) {
   p.tokens = qd->tokens;
   p.kv_heads = kd->heads;
   p.group = qd->heads / kd->heads;
-  p.segments = 1;
-  p.run = p.tokens;
   p.div_heads = make_fastdiv(p.kv_heads);
   // a workgroup of 256 threads to 32 columns of a state
-  require(product({p.batch, p.kv_heads, kd->head_dim / 32, 256}) <= kMostThreads, "q: too large for one launch");
+  const int64_t heads = product({p.batch, p.kv_heads});
+  require(product({heads, kd->head_dim / 32, 256}) <= kMostThreads, "q: too large for one launch");
+  if (p.tokens <= 8) return p;
+  // two workgroups to a compute unit, and runs of two chunks or more
+  const int chunk = linear_chunk(qd->dtype);
+  const int64_t chunks = (int64_t(p.tokens) + chunk - 1) / chunk;
+  const int64_t runs = std::max<int64_t>(1, std::min<int64_t>(512 / heads, chunks / 2));
+  const int64_t each = (chunks + runs - 1) / runs;
+  p.run = (int32_t)(each * chunk);
+  p.segments = (int32_t)((chunks + each - 1) / each);
   return p;
 }
-uint64_t workspace_of(const LinearParams&, int) { return 0; }
+uint64_t workspace_of(const LinearParams& p, int head_dim) {
+  return p.segments <= 1 ? 0 : uint64_t(p.batch) * p.kv_heads * p.segments * (head_dim * head_dim + 1) * 4;
+}
 
 }  // namespace
 

@@ -89,10 +89,13 @@ struct LinearParams {
   int32_t batch, tokens, kv_heads, group;
   float scale;
   FastDiv div_heads;
-  int32_t segments;  // runs of tokens that workgroups of their own take
-  int32_t run;       // tokens of a run
-  float* ws;
+  int32_t segments;  // runs of tokens that workgroups of their own take; 0: token after token
+  int32_t run;       // tokens of a run, whole chunks
+  float* ws;         // segments > 1: [head][run] states, then what runs keep of one
 };
+
+// tokens of a chunk of linear attention
+constexpr int linear_chunk(int dtype) { return dtype == DT_BF16 ? 64 : 32; }
 
 // tokens of a step over the 4-bit cache, and over bf16 and fp32 keys and values
 constexpr int kKvTile = 32, kBf16Tile = 64, kF32Tile = 32;
