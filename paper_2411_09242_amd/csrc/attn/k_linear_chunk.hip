@@ -8,12 +8,12 @@
 // size, and weights between tokens are never above what the decays between them
 // make.
 //
-// A workgroup has one kv head's run of tokens.  Its wavefronts have 32 or 16
-// columns (channels of the values) of S each, in the registers of the matrix
-// cores' results; which rows of S a tile has is chosen so that these registers
-// are the second operand of S^T q as they are, and likewise the products k_j q_i
-// the first one of the sum over j.  They alone go through LDS: every wavefront
-// makes those of some rows.
+// A workgroup has one kv head's run of tokens.  Its wavefronts have 16 columns
+// (channels of the values) of S each, in the registers of the matrix cores'
+// results; which rows of S a tile has is chosen so that these registers
+// are an operand of S^T q as they are, and likewise the products k_j q_i one of
+// the sum over j.  They alone go through LDS: every wavefront makes those of some
+// rows.  The next chunk's tensors are on their way meanwhile.
 //
 // Where there are too few heads to fill the GPU, runs of tokens go to workgroups of
 // their own: a first launch makes what each run adds to a state, and the second
@@ -65,7 +65,7 @@ struct Core;
 
 template <int D>
 struct Core<uint16_t, D> {
-  static constexpr int C = 64, KS = 32, LD = D + 8;  // tokens of a chunk; a row's elements in LDS
+  static constexpr int C = 64, KS = 32, LD = D + 24;  // tokens of a chunk; a row's elements in LDS: 12 banks apart
   static constexpr int PS = 2, PP = 2, PV = 3;       // parts of S, of the weighted products, of v
   typedef u32x4 Frag;
   __device__ static __forceinline__ f32x4 mma(Frag a, Frag b, f32x4 c) {
@@ -114,6 +114,12 @@ struct Core<uint16_t, D> {
       v[i] &= ((v[i] & 0x7f80u) == 0x7f80u ? 0u : 0xffffu) | ((v[i] & 0x7f800000u) == 0x7f800000u ? 0u : 0xffff0000u);
     return v;
   }
+  __device__ static __forceinline__ bool odd(u32x4 v) {
+    bool any = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) any |= (v[i] & 0x7f80u) == 0x7f80u | (v[i] & 0x7f800000u) == 0x7f800000u;
+    return any;
+  }
   __device__ static __forceinline__ float element(const Frag f[PP], int e) {
     float x = 0.0f;
 #pragma unroll
@@ -152,49 +158,69 @@ struct Core<float, D> {
     for (int i = 0; i < 4; ++i) v[i] = odd_value(v[i]) ? 0.0f : v[i];
     return v;
   }
+  __device__ static __forceinline__ bool odd(u32x4 v) {
+    bool any = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) any |= (v[i] & 0x7f800000u) == 0x7f800000u;
+    return any;
+  }
   __device__ static __forceinline__ float element(const Frag f[PP], int e) { return f[0][e]; }
 };
 
-constexpr int linear_waves(int D) { return D == 32 ? 2 : 4; }
+// Waits for this wavefront's own LDS accesses and for the other wavefronts; loads
+// and stores of memory stay in flight.
+__device__ __forceinline__ void lds_barrier() {
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+constexpr int linear_waves(int D) { return D / 16; }
 
 // STATES: the first of two launches, what runs add to a state.
-template <typename T, int D, bool STATES>
-__global__ __launch_bounds__(64 * linear_waves(D), 2) void linear_chunk_kernel(LinearParams p) {
+// VEC: rows start on 16-byte addresses, and a chunk's lie within 32-bit offsets.
+template <typename T, int D, bool STATES, bool VEC>
+__global__ __launch_bounds__(64 * linear_waves(D)) __attribute__((amdgpu_waves_per_eu(4, 4))) void linear_chunk_kernel(
+    LinearParams p) {
   typedef Core<T, D> At;
   typedef typename At::Frag Frag;
-  constexpr int NW = linear_waves(D), THREADS = 64 * NW, NT = D / 16 / NW, MT = D / 16;
+  constexpr int NW = linear_waves(D), THREADS = 64 * NW, MT = D / 16;
   constexpr int C = At::C, KS = At::KS, LD = At::LD, IT = C / 16, TPK = KS / 16, STEPS = D / KS, KSTEPS = C / KS;
+  constexpr int E = 16 / sizeof(T), PIECES = C * D / E / THREADS;  // elements of 16 bytes; pieces of a thread
+  // tiles of 16 rows i times steps of tokens j, those that some j <= i has: step
+  // 0 of all, then step 1 of the later ones
+  static_assert(KSTEPS == 2, "two steps to a chunk");
+  constexpr int UNITS = 2 * IT - TPK;
+  auto unit = [](int it, int ks) { return ks ? IT + it - TPK : it; };
   __shared__ __attribute__((aligned(16))) T sk[C * LD], sv[C * LD], sq[STATES ? 8 : C * LD];
-  __shared__ Frag sp[STATES ? 1 : IT * KSTEPS * At::PP * 64];
-  __shared__ __attribute__((aligned(16))) double sum[C];      // c_i, in powers of two
-  __shared__ __attribute__((aligned(16))) float from[C], to[C];  // 2^{c_i}, 2^{c_C - c_i}
-  __shared__ float kept;                                       // 2^{c_C}
+  __shared__ Frag sp[STATES ? 1 : UNITS * At::PP * 64];
+  // of this and the next chunk in turn: c_i in powers of two, 2^{c_i}, 2^{c_C - c_i}, 2^{c_C}
+  __shared__ __attribute__((aligned(16))) double sum[2][C];
+  __shared__ __attribute__((aligned(16))) float from[2][C], to[2][C];
+  __shared__ float kept[2];
+  __shared__ int odd_at;  // the latest chunk with a value that is no number
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
   const int x = blockIdx.x, seg = blockIdx.y;
   const int b = (int)fdiv(x, p.div_heads), h = x - b * p.kv_heads;
   const int n = clamp_len(p.count, b, p.tokens);
   const int first = seg * p.run, past = min(first + p.run, n);
-  const int col0 = wave * (16 * NT);
+  const int col0 = 16 * wave;
   float* const slots = p.ws + (int64_t)x * p.segments * (D * D);
   float* const decays = p.ws + (int64_t)gridDim.x * p.segments * (D * D) + (int64_t)x * p.segments;
-  auto place = [&](int mt, int nt) { return (((wave * MT + mt) * NT + nt) * 64 + lane) * 4; };
+  const int place = (wave * MT * 64 + lane) * 4;
 
-  f32x4 S[MT][NT];
-  auto given = [&](const float* state) {  // of the caller
+  f32x4 S[MT];
+  auto given = [&](const float* state) {  // by the caller
+    const float* const at = state + (int64_t)x * D * D + At::channel(0, g) * D + col0 + r;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          S[mt][nt][e] = state ? state[(int64_t)x * D * D + (At::channel(mt, g) + e) * D + col0 + 16 * nt + r] : 0.0f;
+      for (int e = 0; e < 4; ++e) S[mt][e] = state ? at[(At::channel(mt, 0) + e) * D] : 0.0f;
   };
   auto keep_slot = [&](int i) {
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) *(f32x4*)(slots + (int64_t)i * (D * D) + place(mt, nt)) = S[mt][nt];
+    for (int mt = 0; mt < MT; ++mt) *(f32x4*)(slots + (int64_t)i * (D * D) + place + 256 * mt) = S[mt];
   };
   if (STATES) {
     // the last run's share is not needed: its place has the state to start from,
@@ -212,16 +238,11 @@ __global__ __launch_bounds__(64 * linear_waves(D), 2) void linear_chunk_kernel(L
     } else {
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-          S[mt][nt] = p.state ? *(const f32x4*)(slots + (int64_t)(p.segments - 1) * (D * D) + place(mt, nt)) : f32x4{};
+        S[mt] = p.state ? *(const f32x4*)(slots + (int64_t)(p.segments - 1) * (D * D) + place + 256 * mt) : f32x4{};
       for (int i = 0; i < seg; ++i) {
         const float a = decays[i];
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-            S[mt][nt] = S[mt][nt] * a + *(const f32x4*)(slots + (int64_t)i * (D * D) + place(mt, nt));
+        for (int mt = 0; mt < MT; ++mt) S[mt] = S[mt] * a + *(const f32x4*)(slots + (int64_t)i * (D * D) + place + 256 * mt);
       }
     }
   }
@@ -229,218 +250,245 @@ __global__ __launch_bounds__(64 * linear_waves(D), 2) void linear_chunk_kernel(L
 
   const T* const k = (const T*)p.k.p + b * p.k.sb + h * p.k.sh;
   const T* const v = (const T*)p.v.p + b * p.v.sb + h * p.v.sh;
+  const T* const q = (const T*)p.q.p + b * p.q.sb + (int64_t)h * p.group * p.q.sh;
   const float* const decay = p.decay + b * p.gb + h * p.gh;
-  // rows t0 .. of a tensor into LDS, zeros behind the last; whether one is no number
-  auto stage = [&](const T* m, const TokensArg& a, int t0, int rows, T* s) {
-    bool odd = false;
-#pragma unroll
-    for (int i = 0; i < C * D / 8 / THREADS; ++i) {
-      const int at = tid + THREADS * i, t = at / (D / 8), c = at % (D / 8) * 8;
-      Eight<T> e;
-      float f[8] = {};
-      if (t < rows) {
-        e.load(m + (int64_t)(t0 + t) * a.st + c, a.vec);
-        e.floats(f);
-      }
-#pragma unroll
-      for (int j = 0; j < 8; ++j) odd |= odd_value(f[j]);
-      store8(s + t * LD + c, true, f);
-    }
-    return odd;
+  // a chunk of a tensor on its way to LDS, zeros behind the last token
+  struct Stage {
+    u32x4 piece[PIECES];
   };
-  double total = 0.0;  // of the run's log decays
-
-  for (int t0 = first; t0 < past; t0 += C) {
-    const int rows = min(C, past - t0);
-    __syncthreads();  // the chunk before is done with LDS
-    stage(k, p.k, t0, rows, sk);
-    const bool odd = stage(v, p.v, t0, rows, sv);
-    if (wave == 0) {
-      double c = 0.0;
-      if (lane < rows) {
-        const float gt = decay[(int64_t)(t0 + lane) * p.gt];
-        c = (gt < -200.0f ? -200.0 : (double)gt) * 1.4426950408889634;
-      }
+  constexpr int ACROSS = D / E, ROWS = THREADS / ACROSS;  // pieces of a row; rows that the threads take at once
+  const int row = tid / ACROSS, piece = tid % ACROSS * E;
+  auto fetch = [&](const T* m, const TokensArg& a, int t0, Stage& to) {
+    const uint32_t at = (uint32_t)(row * (int)a.st + piece) * sizeof(T);
 #pragma unroll
-      for (int m = 1; m < 64; m <<= 1) {
-        const double o = __shfl_up(c, m);
-        if (lane >= m) c += o;
+    for (int i = 0; i < PIECES; ++i) {
+      const T* const base = m + (int64_t)(t0 + ROWS * i) * a.st;
+      to.piece[i] = u32x4{};
+      if (t0 + ROWS * i + row < past) {
+        if constexpr (VEC) {
+          to.piece[i] = *(const u32x4*)((const char*)base + at);
+        } else {
+          const T* const from = base + row * a.st + piece;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if constexpr (sizeof(T) == 2) to.piece[i][e] = from[2 * e] | ((uint32_t)from[2 * e + 1] << 16);
+            else to.piece[i][e] = __float_as_uint(from[e]);
+          }
+        }
       }
-      const double all = __shfl(c, 63);
-      total += all;
-      if (lane < C) {
-        sum[lane] = c;
-        from[lane] = __builtin_amdgcn_exp2f((float)c);
-        to[lane] = __builtin_amdgcn_exp2f((float)(all - c));
-      }
-      const float a = (float)exp2(all);  // every chunk's rounding stays in S
-      if (lane == 0) kept = a;
     }
-    const bool dirty = __syncthreads_or(odd);
+  };
+  auto put = [&](const Stage& from, T* s) {
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) *(u32x4*)(s + (row + ROWS * i) * LD + piece) = from.piece[i];
+  };
+  double total = 0.0;  // of the run's log decays; the last wavefront's
+  auto weights = [&](int t0, int turn) {
+    double c = 0.0;
+    if (lane < C && t0 + lane < past) {
+      const float gt = decay[(int64_t)(t0 + lane) * p.gt];
+      c = (gt < -200.0f ? -200.0 : (double)gt) * 1.4426950408889634;
+    }
+#pragma unroll
+    for (int m = 1; m < C; m <<= 1) {
+      const double o = __shfl_up(c, m);
+      if (lane >= m) c += o;
+    }
+    const double all = __shfl(c, C - 1);
+    if (STATES) total += all;
+    if (lane < C) {
+      sum[turn][lane] = c;
+      from[turn][lane] = __builtin_amdgcn_exp2f((float)c);
+      to[turn][lane] = __builtin_amdgcn_exp2f((float)(all - c));
+    }
+    const float a = (float)exp2(all);  // every chunk's rounding stays in S
+    if (lane == 0) kept[turn] = a;
+  };
 
+  Stage ks_, vs_, qs_;
+  if (first < past) {
+    fetch(k, p.k, first, ks_);
+    fetch(v, p.v, first, vs_);
+    if (!STATES) fetch(q, p.q, first, qs_);
+    if (wave == NW - 1) weights(first, 0);
+    if (tid == 0) odd_at = -1;
+    lds_barrier();
+  }
+  int turn = 0;
+  for (int t0 = first; t0 < past; t0 += C, turn ^= 1) {
+    lds_barrier();  // the chunk before is done with LDS
+    put(ks_, sk);
+    put(vs_, sv);
     if constexpr (!STATES) {
+      put(qs_, sq);
+      bool odd = false;
+#pragma unroll
+      for (int i = 0; i < PIECES; ++i) odd |= At::odd(vs_.piece[i]);
+      if (odd) odd_at = t0;
+    }
+    lds_barrier();
+    const bool more = t0 + C < past;
+    if (more) {
+      fetch(k, p.k, t0 + C, ks_);
+      fetch(v, p.v, t0 + C, vs_);
+    }
+    if constexpr (STATES) {
+      if (more && wave == NW - 1) weights(t0 + C, turn ^ 1);
+    } else {
+      const bool dirty = odd_at == t0;
       for (int j = 0; j < p.group; ++j) {
-        const int64_t head = (int64_t)h * p.group + j;
-        if (j) __syncthreads();  // the head before is done with sq and sp
-        stage((const T*)p.q.p + b * p.q.sb + head * p.q.sh, p.q, t0, rows, sq);
-        __syncthreads();
-        // k_j q_i of the rows i of some tiles, token j in a lane's registers
-        for (int it = wave; it < IT; it += NW) {
+        const bool other = j + 1 < p.group;
+        // not one for all heads: the parts of S would be held beside it
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) asm volatile("" : "+v"(S[mt]));
+        if (other) fetch(q + (j + 1) * p.q.sh, p.q, t0, qs_);
+        else if (more) fetch(q, p.q, t0 + C, qs_);
+        // k_j q_i with its decay: row i to a lane's r, tokens j in its registers
+        for (int u = wave; u < UNITS; u += NW) {
+          const int ks = u >= IT, it = ks ? u - IT + TPK : u;
           Frag qf[STEPS];
 #pragma unroll
           for (int s = 0; s < STEPS; ++s) qf[s] = At::rows(sq, 16 * it + r, s, g);
-          const double ci = sum[16 * it + r];
+          const double ci = sum[turn][16 * it + r];
+          f32x4 w[TPK];
 #pragma unroll
-          for (int ks = 0; ks < KSTEPS; ++ks) {
-            if (ks * KS > 16 * it + 15) break;
-            f32x4 w[TPK];
+          for (int i = 0; i < TPK; ++i) {
+            const int jt = ks * TPK + i;
+            w[i] = f32x4{};
+            if (jt > it) continue;
 #pragma unroll
-            for (int u = 0; u < TPK; ++u) {
-              const int jt = ks * TPK + u;
-              w[u] = f32x4{};
-              if (jt > it) continue;
+            for (int s = 0; s < STEPS; ++s) w[i] = At::mma(At::rows(sk, 16 * jt + r, s, g), qf[s], w[i]);
 #pragma unroll
-              for (int s = 0; s < STEPS; ++s) w[u] = At::mma(At::rows(sk, 16 * jt + r, s, g), qf[s], w[u]);
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const int tj = 16 * jt + 4 * g + e;
-                const float f = __builtin_amdgcn_exp2f((float)(ci - sum[tj])) * w[u][e];
-                w[u][e] = tj <= 16 * it + r ? f : 0.0f;
-              }
+            for (int e = 0; e < 4; ++e) {
+              const int tj = 16 * jt + 4 * g + e;
+              const float f = __builtin_amdgcn_exp2f((float)(ci - sum[turn][tj])) * w[i][e];
+              w[i][e] = tj <= 16 * it + r ? f : 0.0f;
             }
-            Frag f[At::PP];
-            At::template parts<At::PP>(w, 1, f);
-#pragma unroll
-            for (int k = 0; k < At::PP; ++k) sp[((it * KSTEPS + ks) * At::PP + k) * 64 + lane] = f[k];
           }
+          Frag f[At::PP];
+          At::template parts<At::PP>(w, 1, f);
+#pragma unroll
+          for (int i = 0; i < At::PP; ++i) sp[(u * At::PP + i) * 64 + lane] = f[i];
         }
-        __syncthreads();
-        f32x4 o[IT][NT] = {};
+        if (j == 0 && more && wave == NW - 1) weights(t0 + C, turn ^ 1);
+        lds_barrier();
+        f32x4 o[IT] = {};  // channels col0 + 4 g .. + 3 of token 16 it + r
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
-          Frag f[NT][At::PS];
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) At::template parts<At::PS>(&S[s * TPK][nt], NT, f[nt]);
+          Frag f[At::PS];
+          At::template parts<At::PS>(&S[s * TPK], 1, f);
 #pragma unroll
           for (int it = 0; it < IT; ++it) {
             const Frag a = At::rows(sq, 16 * it + r, s, g);
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-              for (int k = 0; k < At::PS; ++k) o[it][nt] = At::mma(a, f[nt][k], o[it][nt]);
+            for (int i = 0; i < At::PS; ++i) o[it] = At::mma(f[i], a, o[it]);
           }
         }
 #pragma unroll
-        for (int it = 0; it < IT; ++it) {
-          const f32x4 e = *(const f32x4*)(from + 16 * it + 4 * g);
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) o[it][nt] *= e;
-        }
+        for (int it = 0; it < IT; ++it) o[it] *= from[turn][16 * it + r];
 #pragma unroll
         for (int ks = 0; ks < KSTEPS; ++ks) {
-          Frag f[NT];
+          // 0 times a later value that is no number would still be none: where a
+          // row's tokens and later ones share a step, such values are left out and
+          // added below
+          const Frag f = At::values(sv, ks, col0, lane);
+          Frag own = f;
+          if (__builtin_expect(dirty, 0)) own = At::clean(f);
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) f[nt] = At::values(sv, ks, col0 + 16 * nt, lane);
+          for (int it = ks * TPK; it < IT; ++it)
 #pragma unroll
-          for (int it = 0; it < IT; ++it) {
-            if (16 * it + 15 < ks * KS) continue;
-            // 0 times a later value that is no number would still be none: where a
-            // row's tokens and later ones share a step, such values are left out
-            // and added below
-            const bool shared = 16 * it + 15 < (ks + 1) * KS;
-            Frag a[At::PP];
-#pragma unroll
-            for (int k = 0; k < At::PP; ++k) a[k] = sp[((it * KSTEPS + ks) * At::PP + k) * 64 + lane];
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-              for (int k = 0; k < At::PP; ++k)
-                o[it][nt] = At::mma(a[k], shared && dirty ? At::clean(f[nt]) : f[nt], o[it][nt]);
-          }
+            for (int i = 0; i < At::PP; ++i)
+              o[it] = At::mma(it < (ks + 1) * TPK ? own : f, sp[(unit(it, ks) * At::PP + i) * 64 + lane], o[it]);
         }
         if (__builtin_expect(dirty, 0)) {
 #pragma unroll
           for (int it = 0; it < IT; ++it) {
-            const int ks = 16 * it / KS;
+            const int ks = it / TPK;
 #pragma nounroll
-            for (int t = ks * KS; t < min((ks + 1) * KS, 16 * it + 16); ++t)
+            for (int t = ks * KS; t < 16 * it + 16; ++t) {
+              Frag a[At::PP];
 #pragma unroll
-              for (int nt = 0; nt < NT; ++nt) {
-                const float val = Elem<T>::load(sv, t * LD + col0 + 16 * nt + r);
-                if (!odd_value(val)) continue;
+              for (int i = 0; i < At::PP; ++i) a[i] = sp[(unit(it, ks) * At::PP + i) * 64 + 16 * ((t & 15) >> 2) + r];
+              const float w = At::element(a, 4 * ((t % KS) >> 4) + (t & 3));
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                  const int i = 16 * it + 4 * g + e;
-                  if (t > i) continue;
-                  Frag a[At::PP];
-#pragma unroll
-                  for (int k = 0; k < At::PP; ++k)
-                    a[k] = sp[((it * KSTEPS + ks) * At::PP + k) * 64 + 16 * ((t & 15) >> 2) + (i & 15)];
-                  o[it][nt][e] += At::element(a, 4 * ((t % KS) >> 4) + (t & 3)) * val;
-                }
+              for (int e = 0; e < 4; ++e) {
+                const float val = Elem<T>::load(sv, t * LD + col0 + 4 * g + e);
+                if (odd_value(val) && t <= 16 * it + r) o[it][e] += w * val;
               }
+            }
           }
         }
-        T* const out = (T*)p.o.p + b * p.o.sb + head * p.o.sh;
+        T* const out = (T*)p.o.p + b * p.o.sb + ((int64_t)h * p.group + j) * p.o.sh + col0;
+        const uint32_t to = (uint32_t)(r * (int)p.o.st + 4 * g) * sizeof(T);
 #pragma unroll
-        for (int it = 0; it < IT; ++it)
+        for (int it = 0; it < IT; ++it) {
+          const int t = t0 + 16 * it;
+          if (t + r >= past) continue;
+          T* const base = out + (int64_t)t * p.o.st;
+          const f32x4 y = o[it] * p.scale;
+          if constexpr (VEC) {
+            char* const at = (char*)base + to;
+            if constexpr (sizeof(T) == 2) *(uint2*)at = make_uint2(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
+            else *(f32x4*)at = y;
+          } else {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int i = 16 * it + 4 * g + e;
-            if (i >= rows) continue;
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-              Elem<T>::store(out + (int64_t)(t0 + i) * p.o.st, col0 + 16 * nt + r, p.scale * o[it][nt][e]);
+            for (int e = 0; e < 4; ++e) Elem<T>::store(base + r * p.o.st + 4 * g, e, y[e]);
           }
+        }
+        if (other) {
+          lds_barrier();  // this head is done with sq and sp
+          put(qs_, sq);
+          lds_barrier();
+        }
       }
-      if (t0 + C >= past && !(last && p.state_out)) break;  // nobody reads this state
+      if (!more && !(last && p.state_out)) break;  // nobody reads this state
     }
 
-    const float a = kept;
+    const float a = kept[turn];
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) S[mt][nt] *= a;
+    for (int mt = 0; mt < MT; ++mt) S[mt] *= a;
 #pragma unroll
     for (int ks = 0; ks < KSTEPS; ++ks) {
-      Frag f[NT][At::PV];
-      const f32x4 w0 = *(const f32x4*)(to + KS * ks + 4 * g), w1 = *(const f32x4*)(to + KS * ks + (KS - 16) + 4 * g);
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) At::template weigh<At::PV>(At::values(sv, ks, col0 + 16 * nt, lane), w0, w1, f[nt]);
+      Frag f[At::PV];
+      const f32x4 w0 = *(const f32x4*)(to[turn] + KS * ks + 4 * g), w1 = *(const f32x4*)(to[turn] + KS * ks + (KS - 16) + 4 * g);
+      At::template weigh<At::PV>(At::values(sv, ks, col0, lane), w0, w1, f);
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) {
         const Frag kt = At::keys(sk, ks, mt, lane);
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int i = 0; i < At::PV; ++i) S[mt][nt] = At::mma(kt, f[nt][i], S[mt][nt]);
+        for (int i = 0; i < At::PV; ++i) S[mt] = At::mma(kt, f[i], S[mt]);
       }
     }
   }
   if (STATES) {
     keep_slot(seg);
-    if (tid == 0) decays[seg] = (float)exp2(total);
+    if (tid == THREADS - 64) decays[seg] = (float)exp2(total);
   } else if (last && p.state_out) {
+    float* const at = p.state_out + (int64_t)x * D * D + At::channel(0, g) * D + col0 + r;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          p.state_out[(int64_t)x * D * D + (At::channel(mt, g) + e) * D + col0 + 16 * nt + r] = S[mt][nt][e];
+      for (int e = 0; e < 4; ++e) at[(At::channel(mt, 0) + e) * D] = S[mt][e];
   }
+}
+
+template <typename T, int D, bool VEC>
+hipError_t launch(const LinearParams& p, hipStream_t s) {
+  const dim3 grid((uint32_t)(p.batch * p.kv_heads), p.segments), block(64 * linear_waves(D));
+  if (p.segments > 1) {
+    hipLaunchKernelGGL((linear_chunk_kernel<T, D, true, VEC>), grid, block, 0, s, p);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL((linear_chunk_kernel<T, D, false, VEC>), grid, block, 0, s, p);
+  return hipGetLastError();
 }
 
 template <typename T, int D>
 hipError_t launch(const LinearParams& p, hipStream_t s) {
-  const dim3 grid((uint32_t)(p.batch * p.kv_heads), p.segments), block(64 * linear_waves(D));
-  if (p.segments > 1) {
-    hipLaunchKernelGGL((linear_chunk_kernel<T, D, true>), grid, block, 0, s, p);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
-  hipLaunchKernelGGL((linear_chunk_kernel<T, D, false>), grid, block, 0, s, p);
-  return hipGetLastError();
+  const int64_t most = (int64_t(1) << 31) / 256 - D;  // 64 rows of 4 bytes an element
+  const bool vec = p.q.vec && p.k.vec && p.v.vec && p.o.vec && p.q.st < most && p.k.st < most && p.v.st < most && p.o.st < most;
+  return vec ? launch<T, D, true>(p, s) : launch<T, D, false>(p, s);
 }
 
 template <typename T>
