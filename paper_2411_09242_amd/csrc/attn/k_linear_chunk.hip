@@ -120,12 +120,6 @@ struct Core<uint16_t, D> {
     for (int i = 0; i < 4; ++i) any |= (v[i] & 0x7f80u) == 0x7f80u | (v[i] & 0x7f800000u) == 0x7f800000u;
     return any;
   }
-  __device__ static __forceinline__ float element(const Frag f[PP], int e) {
-    float x = 0.0f;
-#pragma unroll
-    for (int k = 0; k < PP; ++k) x += __uint_as_float(e & 1 ? f[k][e >> 1] & 0xffff0000u : f[k][e >> 1] << 16);
-    return x;
-  }
 };
 
 template <int D>
@@ -164,8 +158,15 @@ struct Core<float, D> {
     for (int i = 0; i < 4; ++i) any |= (v[i] & 0x7f800000u) == 0x7f800000u;
     return any;
   }
-  __device__ static __forceinline__ float element(const Frag f[PP], int e) { return f[0][e]; }
 };
+
+// 2^c, with what fp32 cuts off of c: what a chunk keeps of a state is used as
+// often as there are chunks.  (exp2 of a double has some forty registers of
+// constants, held for the whole loop.)
+__device__ __forceinline__ float power_of_two(double c) {
+  const float hi = (float)c, e = __builtin_amdgcn_exp2f(hi);
+  return __builtin_fmaf(e, (float)(c - hi) * 0.69314718f, e);
+}
 
 // Waits for this wavefront's own LDS accesses and for the other wavefronts; loads
 // and stores of memory stay in flight.
@@ -175,11 +176,34 @@ __device__ __forceinline__ void lds_barrier() {
   asm volatile("" ::: "memory");
 }
 
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double add_dpp(double v) {
+  const int64_t x = __double_as_longlong(v);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)x, CTRL, ROWS, 0xf, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(x >> 32), CTRL, ROWS, 0xf, false);
+  return v + __longlong_as_double((int64_t)((uint64_t)hi << 32 | lo));
+}
+// The sums up to each lane, and the last one's.
+__device__ __forceinline__ double wave_scan(double v) {
+  v = add_dpp<0x111, 0xf>(v);  // from the lane 1, 2, 4, 8 before it in its row of 16
+  v = add_dpp<0x112, 0xf>(v);
+  v = add_dpp<0x114, 0xf>(v);
+  v = add_dpp<0x118, 0xf>(v);
+  v = add_dpp<0x142, 0xa>(v);  // a row's last lane to the next row
+  return add_dpp<0x143, 0xc>(v);  // lane 31 to the upper rows
+}
+__device__ __forceinline__ double last_lane(double v) {
+  const int64_t x = __double_as_longlong(v);
+  const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)x, 63), hi = __builtin_amdgcn_readlane((int)(x >> 32), 63);
+  return __longlong_as_double((int64_t)((uint64_t)hi << 32 | lo));
+}
+
 constexpr int linear_waves(int D) { return D / 16; }
 
 // STATES: the first of two launches, what runs add to a state.
 // VEC: rows start on 16-byte addresses, and a chunk's lie within 32-bit offsets.
-template <typename T, int D, bool STATES, bool VEC>
+// ONE: a query head to a kv head; the loop over them costs registers.
+template <typename T, int D, bool STATES, bool VEC, bool ONE>
 __global__ __launch_bounds__(64 * linear_waves(D)) __attribute__((amdgpu_waves_per_eu(4, 4))) void linear_chunk_kernel(
     LinearParams p) {
   typedef Core<T, D> At;
@@ -252,28 +276,25 @@ __global__ __launch_bounds__(64 * linear_waves(D)) __attribute__((amdgpu_waves_p
   const T* const v = (const T*)p.v.p + b * p.v.sb + h * p.v.sh;
   const T* const q = (const T*)p.q.p + b * p.q.sb + (int64_t)h * p.group * p.q.sh;
   const float* const decay = p.decay + b * p.gb + h * p.gh;
-  // a chunk of a tensor on its way to LDS, zeros behind the last token
+  // a chunk of a tensor on its way to LDS; places behind the last token repeat it
   struct Stage {
     u32x4 piece[PIECES];
   };
   constexpr int ACROSS = D / E, ROWS = THREADS / ACROSS;  // pieces of a row; rows that the threads take at once
   const int row = tid / ACROSS, piece = tid % ACROSS * E;
   auto fetch = [&](const T* m, const TokensArg& a, int t0, Stage& to) {
-    const uint32_t at = (uint32_t)(row * (int)a.st + piece) * sizeof(T);
+    const T* const base = m + (int64_t)t0 * a.st;
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
-      const T* const base = m + (int64_t)(t0 + ROWS * i) * a.st;
-      to.piece[i] = u32x4{};
-      if (t0 + ROWS * i + row < past) {
-        if constexpr (VEC) {
-          to.piece[i] = *(const u32x4*)((const char*)base + at);
-        } else {
-          const T* const from = base + row * a.st + piece;
+      const int t = min(row + ROWS * i, past - 1 - t0);
+      if constexpr (VEC) {
+        to.piece[i] = *(const u32x4*)((const char*)base + (uint32_t)(t * (int)a.st + piece) * sizeof(T));
+      } else {
+        const T* const from = base + t * a.st + piece;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            if constexpr (sizeof(T) == 2) to.piece[i][e] = from[2 * e] | ((uint32_t)from[2 * e + 1] << 16);
-            else to.piece[i][e] = __float_as_uint(from[e]);
-          }
+        for (int e = 0; e < 4; ++e) {
+          if constexpr (sizeof(T) == 2) to.piece[i][e] = from[2 * e] | ((uint32_t)from[2 * e + 1] << 16);
+          else to.piece[i][e] = __float_as_uint(from[e]);
         }
       }
     }
@@ -282,26 +303,25 @@ __global__ __launch_bounds__(64 * linear_waves(D)) __attribute__((amdgpu_waves_p
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) *(u32x4*)(s + (row + ROWS * i) * LD + piece) = from.piece[i];
   };
-  double total = 0.0;  // of the run's log decays; the last wavefront's
+  // The last wavefront makes the next chunk's weights from decays that it has
+  // loaded a chunk before: the others would wait for them.
+  double total = 0.0;  // of the run's log decays
+  float ahead = 0.0f;
+  auto fetch_decay = [&](int t0) {
+    const float gt = decay[(int64_t)min(t0 + (lane & (C - 1)), past - 1) * p.gt];
+    ahead = t0 + lane < past && lane < C ? gt : 0.0f;
+  };
   auto weights = [&](int t0, int turn) {
-    double c = 0.0;
-    if (lane < C && t0 + lane < past) {
-      const float gt = decay[(int64_t)(t0 + lane) * p.gt];
-      c = (gt < -200.0f ? -200.0 : (double)gt) * 1.4426950408889634;
-    }
-#pragma unroll
-    for (int m = 1; m < C; m <<= 1) {
-      const double o = __shfl_up(c, m);
-      if (lane >= m) c += o;
-    }
-    const double all = __shfl(c, C - 1);
+    double c = wave_scan((ahead < -200.0f ? -200.0 : (double)ahead) * 1.4426950408889634);
+    fetch_decay(t0 + C);
+    const double all = last_lane(c);
     if (STATES) total += all;
     if (lane < C) {
       sum[turn][lane] = c;
       from[turn][lane] = __builtin_amdgcn_exp2f((float)c);
       to[turn][lane] = __builtin_amdgcn_exp2f((float)(all - c));
     }
-    const float a = (float)exp2(all);  // every chunk's rounding stays in S
+    const float a = power_of_two(all);
     if (lane == 0) kept[turn] = a;
   };
 
@@ -310,13 +330,18 @@ __global__ __launch_bounds__(64 * linear_waves(D)) __attribute__((amdgpu_waves_p
     fetch(k, p.k, first, ks_);
     fetch(v, p.v, first, vs_);
     if (!STATES) fetch(q, p.q, first, qs_);
-    if (wave == NW - 1) weights(first, 0);
+    if (wave == NW - 1) fetch_decay(first), weights(first, 0);
     if (tid == 0) odd_at = -1;
     lds_barrier();
   }
   int turn = 0;
   for (int t0 = first; t0 < past; t0 += C, turn ^= 1) {
     lds_barrier();  // the chunk before is done with LDS
+    if (past - t0 < C) {  // nothing from behind the last token enters the state
+#pragma unroll
+      for (int i = 0; i < PIECES; ++i)
+        if (row + ROWS * i >= past - t0) vs_.piece[i] = u32x4{};
+    }
     put(ks_, sk);
     put(vs_, sv);
     if constexpr (!STATES) {
@@ -336,8 +361,9 @@ __global__ __launch_bounds__(64 * linear_waves(D)) __attribute__((amdgpu_waves_p
       if (more && wave == NW - 1) weights(t0 + C, turn ^ 1);
     } else {
       const bool dirty = odd_at == t0;
-      for (int j = 0; j < p.group; ++j) {
-        const bool other = j + 1 < p.group;
+      const int heads = ONE ? 1 : p.group;
+      for (int j = 0; j < heads; ++j) {
+        const bool other = j + 1 < heads;
         // not one for all heads: the parts of S would be held beside it
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) asm volatile("" : "+v"(S[mt]));
@@ -401,20 +427,25 @@ __global__ __launch_bounds__(64 * linear_waves(D)) __attribute__((amdgpu_waves_p
               o[it] = At::mma(it < (ks + 1) * TPK ? own : f, sp[(unit(it, ks) * At::PP + i) * 64 + lane], o[it]);
         }
         if (__builtin_expect(dirty, 0)) {
-#pragma unroll
-          for (int it = 0; it < IT; ++it) {
-            const int ks = it / TPK;
 #pragma nounroll
-            for (int t = ks * KS; t < 16 * it + 16; ++t) {
-              Frag a[At::PP];
+          for (int t = 0; t < C; ++t) {
+            float val[4];
+            bool any = false;
 #pragma unroll
-              for (int i = 0; i < At::PP; ++i) a[i] = sp[(unit(it, ks) * At::PP + i) * 64 + 16 * ((t & 15) >> 2) + r];
-              const float w = At::element(a, 4 * ((t % KS) >> 4) + (t & 3));
+            for (int e = 0; e < 4; ++e) val[e] = Elem<T>::load(sv, t * LD + col0 + 4 * g + e), any |= odd_value(val[e]);
+            if (!__any(any)) continue;
+            // of part 0, row r, token t
+            const int at = 16 / (int)sizeof(T) * (16 * ((t & 15) >> 2) + r) + 4 * (t % KS >> 4) + (t & 3);
 #pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const float val = Elem<T>::load(sv, t * LD + col0 + 4 * g + e);
-                if (odd_value(val) && t <= 16 * it + r) o[it][e] += w * val;
-              }
+            for (int it = 0; it < IT; ++it) {
+              if (it / TPK != t / KS) continue;
+              float w = 0.0f;
+#pragma unroll
+              for (int i = 0; i < At::PP; ++i)
+                w += Elem<T>::load(sp, (unit(it, it / TPK) * At::PP + i) * (1024 / (int)sizeof(T)) + at);
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if (t <= 16 * it + r && odd_value(val[e])) o[it][e] += w * val[e];
             }
           }
         }
@@ -462,7 +493,7 @@ __global__ __launch_bounds__(64 * linear_waves(D)) __attribute__((amdgpu_waves_p
   }
   if (STATES) {
     keep_slot(seg);
-    if (tid == THREADS - 64) decays[seg] = (float)exp2(total);
+    if (tid == THREADS - 64) decays[seg] = power_of_two(total);
   } else if (last && p.state_out) {
     float* const at = p.state_out + (int64_t)x * D * D + At::channel(0, g) * D + col0 + r;
 #pragma unroll
@@ -472,15 +503,15 @@ __global__ __launch_bounds__(64 * linear_waves(D)) __attribute__((amdgpu_waves_p
   }
 }
 
-template <typename T, int D, bool VEC>
+template <typename T, int D, bool VEC, bool ONE>
 hipError_t launch(const LinearParams& p, hipStream_t s) {
   const dim3 grid((uint32_t)(p.batch * p.kv_heads), p.segments), block(64 * linear_waves(D));
   if (p.segments > 1) {
-    hipLaunchKernelGGL((linear_chunk_kernel<T, D, true, VEC>), grid, block, 0, s, p);
+    hipLaunchKernelGGL((linear_chunk_kernel<T, D, true, VEC, true>), grid, block, 0, s, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL((linear_chunk_kernel<T, D, false, VEC>), grid, block, 0, s, p);
+  hipLaunchKernelGGL((linear_chunk_kernel<T, D, false, VEC, ONE>), grid, block, 0, s, p);
   return hipGetLastError();
 }
 
@@ -488,7 +519,8 @@ template <typename T, int D>
 hipError_t launch(const LinearParams& p, hipStream_t s) {
   const int64_t most = (int64_t(1) << 31) / 256 - D;  // 64 rows of 4 bytes an element
   const bool vec = p.q.vec && p.k.vec && p.v.vec && p.o.vec && p.q.st < most && p.k.st < most && p.v.st < most && p.o.st < most;
-  return vec ? launch<T, D, true>(p, s) : launch<T, D, false>(p, s);
+  if (!vec) return launch<T, D, false, false>(p, s);
+  return p.group == 1 ? launch<T, D, true, true>(p, s) : launch<T, D, true, false>(p, s);
 }
 
 template <typename T>
