@@ -9,6 +9,7 @@ namespace fluid {
 
 hipError_t launch_w4_pack(const W4Params& p, int dtype, hipStream_t s);
 hipError_t launch_w4_read(const W4Params& p, int dtype, hipStream_t s);
-hipError_t launch_w4_matmul(const W4Params& p, int dtype, hipStream_t s);
+hipError_t launch_w4_few(const W4Params& p, int dtype, hipStream_t s);
+hipError_t launch_w4_rows(const W4Params& p, int dtype, hipStream_t s);
 
 }  // namespace fluid

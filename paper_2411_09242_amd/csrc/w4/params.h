@@ -24,7 +24,13 @@ struct W4Params {
   int64_t xs, as, os;  // their rows' strides in elements
   int32_t m;           // rows of x
   int32_t vec;         // x's rows start on 16-byte addresses
-  int32_t waves;       // wavefronts that share a tile's channels
+  // up to 16 rows
+  int32_t wide;   // two tiles to a workgroup
+  int32_t waves;  // wavefronts that share a tile's channels
+  // more
+  int32_t splits;  // runs of blocks that workgroups of their own take; 0: up to 16 rows
+  int32_t run;     // blocks of a run
+  float* ws;       // splits > 1: [run][matrix][row][output] sums
 };
 
 }  // namespace fluid

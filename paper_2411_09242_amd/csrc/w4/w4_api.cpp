@@ -1,6 +1,7 @@
 // Entry points of fluid_w4.h: argument checks and launch sizes.
 #include "fluid_w4.h"
 
+#include <algorithm>
 #include <cstdint>
 
 #include "../host/handles.h"
@@ -50,6 +51,27 @@ void check_apart(const fluid_matrix* d, const char* name) {
   require(d->rows == 1 || d->stride >= d->cols, name, ": an output's stride must be at least its cols");
 }
 
+// How the channels are shared.
+void plan_product(W4Params& p, int32_t rows, bool gate, int dtype) {
+  p.m = rows;
+  require(rows <= 64 * 65535, "x: too many rows for one launch");
+  require(int64_t(p.tiles) * 1024 < int64_t(1) << 32, "w: too large for one launch");
+  if (rows <= 16) {
+    // wavefronts with blocks of their own
+    p.wide = p.tiles >= 1024 && !gate;
+    p.waves = p.blocks >= 16 && !gate && !p.wide && dtype == FLUID_BF16 ? 16 : p.blocks >= 8 ? 8 : 4;
+    return;
+  }
+  // as many runs as make a workgroup to a compute unit, of four blocks or more
+  const int64_t groups = (int64_t(p.tiles) + 7) / 8 * ((rows + 63) / 64);
+  const int64_t runs = std::max<int64_t>(1, std::min<int64_t>(256 / groups, p.blocks / 4));
+  p.run = (int32_t)((p.blocks + runs - 1) / runs);
+  p.splits = (p.blocks + p.run - 1) / p.run;
+}
+uint64_t workspace_of(const W4Params& p, bool gate) {
+  return p.splits <= 1 ? 0 : uint64_t(p.splits) * (gate ? 2 : 1) * p.m * p.n * 4;
+}
+
 }  // namespace
 
 }  // namespace fluid
@@ -91,9 +113,20 @@ fluid_status fluid_w4_read(const fluid_w4* w, const void* packed, const fluid_ma
   });
 }
 
+fluid_status fluid_w4_matmul_workspace(const fluid_w4* w, int32_t rows, int32_t gated, uint64_t* bytes) {
+  return call_guarded([&] {
+    W4Params p = check_shape(w);
+    require(rows >= 1, "rows must be at least 1");
+    require(gated == 0 || gated == 1, "gated must be 0 or 1");
+    require(bytes != nullptr, "bytes: NULL");
+    plan_product(p, rows, gated, FLUID_BF16);
+    *bytes = workspace_of(p, gated);
+  });
+}
+
 fluid_status fluid_w4_matmul(const fluid_w4* w, const void* packed, const void* gate, const fluid_matrix* xd,
                              const void* x, const fluid_matrix* ad, const void* add, const fluid_matrix* od, void* out,
-                             void* hip_stream) {
+                             void* workspace, uint64_t workspace_bytes, void* hip_stream) {
   return call_guarded([&] {
     W4Params p = check_shape(w);
     p.w = held(p, packed, "packed");
@@ -108,15 +141,19 @@ fluid_status fluid_w4_matmul(const fluid_w4* w, const void* packed, const void* 
       require(add != out || p.as == p.os, "out: where it is add it must have its stride");
     }
     require(out != x, "out must not be x");
-    require(xd->rows <= 64 * 65535, "x: too many rows for one launch");
-    require(int64_t(p.tiles) * 1024 < int64_t(1) << 32, "w: too large for one launch");
+    plan_product(p, xd->rows, gate != nullptr, xd->dtype);
     p.x = x;
     p.add = add;
     p.out = out;
-    p.m = xd->rows;
     p.vec = (uintptr_t)x % 16 == 0 && (p.xs * dtype_bytes(xd->dtype)) % 16 == 0;
-    // wavefronts with blocks of their own; more rows take more registers
-    p.waves = p.blocks >= 16 && p.m <= 16 ? 16 : p.blocks >= 8 ? 8 : 4;
+    const uint64_t need = workspace_of(p, gate != nullptr);
+    if (need) {
+      if (workspace == nullptr || workspace_bytes < need)
+        fail(FLUID_E_ARENA_TOO_SMALL, "workspace: " + std::to_string(need) + " bytes needed, " +
+                                          std::to_string(workspace ? workspace_bytes : 0) + " given");
+      require((uintptr_t)workspace % 256 == 0, "workspace: must be 256-byte aligned");
+      p.ws = (float*)workspace;
+    }
     run_w4_matmul(p, xd->dtype, hip_stream);
   });
 }

@@ -18,7 +18,7 @@ void run_w4_read(const W4Params& p, int dtype, void* stream) {
   check(launch_w4_read(p, dtype, (hipStream_t)stream), "fluid_w4_read");
 }
 void run_w4_matmul(const W4Params& p, int dtype, void* stream) {
-  check(launch_w4_matmul(p, dtype, (hipStream_t)stream), "fluid_w4_matmul");
+  check((p.splits ? launch_w4_rows : launch_w4_few)(p, dtype, (hipStream_t)stream), "fluid_w4_matmul");
 }
 
 }  // namespace fluid

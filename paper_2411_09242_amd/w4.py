@@ -16,7 +16,7 @@ import ctypes as C
 
 from . import fluid
 from .attention import (_addr, _calls, _check_grad, _device_of, _as_stream, _form, _keep, _launch, _raw_stream, _record,
-                        _refuse, _stream, _torch)
+                        _refuse, _stream, _torch, _workspace)
 
 _VP, _I32, _U64 = C.c_void_p, C.c_int32, C.c_uint64
 
@@ -33,7 +33,8 @@ _PROTOS = {
     "fluid_w4_bytes": [_VP] * 2,
     "fluid_w4_pack": [_VP] * 5,
     "fluid_w4_read": [_VP] * 5,
-    "fluid_w4_matmul": [_VP] * 10,
+    "fluid_w4_matmul_workspace": [_VP, _I32, _I32, _VP],
+    "fluid_w4_matmul": [_VP] * 10 + [_U64, _VP],
 }
 SYMBOLS = tuple(_PROTOS)
 
@@ -174,10 +175,24 @@ def _matmul_call(x, w, gate, add, out):
             _refuse(f"add: {shape} is needed, got {tuple(add.shape)}")
     if tuple(out.shape) != shape:
         _refuse(f"out: {shape} is needed, got {tuple(out.shape)}")
-    return (_lib(), dev, _addr(xd), None if ad is None else _addr(ad), _addr(od), (xd, ad, od))
+    need = _need(w, xd.rows, gate is not None)
+    return (_lib(), dev, _addr(xd), None if ad is None else _addr(ad), _addr(od), need, (xd, ad, od))
 
 
-def w4_matmul(x, w, gate=None, add=None, out=None, stream=None):
+def _need(w, rows, gated):
+    n = _U64()
+    fluid._check(_lib().fluid_w4_matmul_workspace(_addr(w.desc), rows, 1 if gated else 0, C.byref(n)))
+    return n.value
+
+
+def w4_matmul_workspace(x, w, gated=False):
+    """Bytes of workspace that ``w4_matmul`` needs for these arguments."""
+    dev = _device_of(x, "x")
+    _check_w4(w, "w", dev)
+    return _need(w, _matrix(x, "x", dev).rows, gated)
+
+
+def w4_matmul(x, w, gate=None, add=None, out=None, workspace=None, stream=None):
     """x W^T for x [.., cols] and the 4-bit matrix w [rows, cols]; with ``gate``, a
     matrix of w's sizes, SiLU(x gate^T) * (x W^T); plus ``add`` [.., rows] if there
     is one.  out may be ``add``; it is allocated by default.  Made for few rows.
@@ -192,10 +207,12 @@ def w4_matmul(x, w, gate=None, add=None, out=None, stream=None):
     made = _calls.get(key)
     if made is None:
         made = _keep(key, _matmul_call(x, w, gate, add, out))
-    lib, dev, xd, ad, od, _ = made
+    lib, dev, xd, ad, od, need, _ = made
+    keep, ws, ws_bytes = _workspace(need, workspace, dev, stream) if need else (None, None, 0)
     _launch(lib.fluid_w4_matmul, dev, C.addressof(w.desc), w.packed.data_ptr(),
             None if gate is None else gate.packed.data_ptr(), xd, x.data_ptr(), ad, None if add is None else add.data_ptr(),
-            od, out.data_ptr(), _raw_stream(dev) if stream is None else _stream(stream, dev))
+            od, out.data_ptr(), ws, ws_bytes, _raw_stream(dev) if stream is None else _stream(stream, dev))
     if stream is not None:
-        _record(stream, dev, x, add, out, w.packed, None if gate is None else gate.packed)
+        _record(stream, dev, x, add, out, w.packed, None if gate is None else gate.packed, workspace)
+    del keep
     return out

@@ -206,9 +206,10 @@ def matrix(rows=3, cols=200, dtype=F.BF16, stride=None):
     return W.Matrix(dtype, rows, cols, cols if stride is None else stride)
 
 
-def matmul(w=None, packed=ADDR, gate=None, xd=None, x=ADDR, ad=None, add=None, od=None, out=ADDR + 65536, no_w=False):
+def matmul(w=None, packed=ADDR, gate=None, xd=None, x=ADDR, ad=None, add=None, od=None, out=ADDR + 65536, no_w=False,
+           ws=ADDR, ws_bytes=1 << 40):
     st = W._lib().fluid_w4_matmul(None if no_w else ref(w or shape()), packed, gate, ref(xd or matrix()), x, ref(ad), add,
-                                  ref(od or matrix(cols=40)), out, None)
+                                  ref(od or matrix(cols=40)), out, ws, ws_bytes, None)
     return st, error()
 
 
@@ -235,6 +236,26 @@ def test_right_products_reach_the_gpu_part():
 def test_product_refusals(bad, word):
     st, msg = matmul(**bad)
     assert st == INVALID and word in msg, (st, msg)
+
+
+def test_product_workspace_is_checked():
+    lib, n = W._lib(), C.c_uint64()
+    w = shape(rows=512, cols=8192)
+    kw = dict(w=w, xd=matrix(rows=40, cols=8192), od=matrix(rows=40, cols=512))
+    assert lib.fluid_w4_matmul_workspace(ref(w), 40, 0, C.byref(n)) == 0 and n.value > 0
+    assert matmul(**kw, ws_bytes=n.value)[0] == UNSUPPORTED
+    for bad in (dict(ws_bytes=n.value - 1), dict(ws=None)):
+        st, msg = matmul(**kw, **bad)
+        assert st == TOO_SMALL and "workspace" in msg
+    st, msg = matmul(**kw, ws=ADDR + 16)
+    assert st == INVALID and "aligned" in msg
+    assert lib.fluid_w4_matmul_workspace(ref(w), 40, 1, C.byref(n)) == 0 and matmul(**kw, gate=ADDR, ws_bytes=n.value)[0] == UNSUPPORTED
+    assert lib.fluid_w4_matmul_workspace(ref(w), 16, 0, C.byref(n)) == 0 and n.value == 0
+    kw = dict(w=w, xd=matrix(rows=16, cols=8192), od=matrix(rows=16, cols=512))
+    assert matmul(**kw, ws=None, ws_bytes=0)[0] == UNSUPPORTED
+    for bad in ((w, 0, 0), (w, 40, 2), (shape(group=5), 40, 0)):
+        assert lib.fluid_w4_matmul_workspace(ref(bad[0]), bad[1], bad[2], C.byref(n)) == INVALID
+    assert lib.fluid_w4_matmul_workspace(ref(w), 40, 0, None) == INVALID
 
 
 def test_packing_and_reading_refusals():
