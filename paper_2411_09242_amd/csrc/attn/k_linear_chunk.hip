@@ -8,14 +8,16 @@
 // size, and weights between tokens are never above what the decays between them
 // make.
 //
-// A workgroup has one kv head's run of tokens.  Its wavefronts have 16 columns
+// A workgroup has one query head's run of tokens.  Its wavefronts have 16 columns
 // (channels of the values) of S each, in the registers of the matrix cores'
 // results; which rows of S a tile has is chosen so that these registers
 // are an operand of S^T q as they are, and likewise the products k_j q_i one of
 // the sum over j.  They alone go through LDS: every wavefront makes those of some
 // rows.  The next chunk's tensors are on their way meanwhile.
 //
-// Where there are too few heads to fill the GPU, runs of tokens go to workgroups of
+// The query heads of a kv head make the same states: sharing them in a workgroup
+// took a loop over the heads, registers that the compiler spilled, and longer
+// runs.  Where there are too few heads to fill the GPU, runs of tokens go to workgroups of
 // their own: a first launch makes what each run adds to a state, and the second
 // one's workgroups fold those before their run, in order.
 //
@@ -202,8 +204,7 @@ constexpr int linear_waves(int D) { return D / 16; }
 
 // STATES: the first of two launches, what runs add to a state.
 // VEC: rows start on 16-byte addresses, and a chunk's lie within 32-bit offsets.
-// ONE: a query head to a kv head; the loop over them costs registers.
-template <typename T, int D, bool STATES, bool VEC, bool ONE>
+template <typename T, int D, bool STATES, bool VEC>
 __global__ __launch_bounds__(64 * linear_waves(D)) __attribute__((amdgpu_waves_per_eu(4, 4))) void linear_chunk_kernel(
     LinearParams p) {
   typedef Core<T, D> At;
@@ -225,7 +226,7 @@ __global__ __launch_bounds__(64 * linear_waves(D)) __attribute__((amdgpu_waves_p
   __shared__ int odd_at;  // the latest chunk with a value that is no number
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
-  const int x = blockIdx.x, seg = blockIdx.y;
+  const int x = blockIdx.x, seg = blockIdx.y, j = blockIdx.z;  // kv head, run, query head of the group
   const int b = (int)fdiv(x, p.div_heads), h = x - b * p.kv_heads;
   const int n = clamp_len(p.count, b, p.tokens);
   const int first = seg * p.run, past = min(first + p.run, n);
@@ -254,27 +255,14 @@ __global__ __launch_bounds__(64 * linear_waves(D)) __attribute__((amdgpu_waves_p
       return;
     }
     if (past <= first) return;
-    given(nullptr);
   } else {
     if (past <= first && seg > 0) return;
-    if (p.segments == 1) {
-      given(p.state);
-    } else {
-#pragma unroll
-      for (int mt = 0; mt < MT; ++mt)
-        S[mt] = p.state ? *(const f32x4*)(slots + (int64_t)(p.segments - 1) * (D * D) + place + 256 * mt) : f32x4{};
-      for (int i = 0; i < seg; ++i) {
-        const float a = decays[i];
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) S[mt] = S[mt] * a + *(const f32x4*)(slots + (int64_t)i * (D * D) + place + 256 * mt);
-      }
-    }
   }
-  const bool last = past == n || p.segments == 1;  // its state is the last one
+  const bool last = j == 0 && past == n && p.state_out;  // its state is the last one
 
   const T* const k = (const T*)p.k.p + b * p.k.sb + h * p.k.sh;
   const T* const v = (const T*)p.v.p + b * p.v.sb + h * p.v.sh;
-  const T* const q = (const T*)p.q.p + b * p.q.sb + (int64_t)h * p.group * p.q.sh;
+  const T* const q = (const T*)p.q.p + b * p.q.sb + ((int64_t)h * p.group + j) * p.q.sh;
   const float* const decay = p.decay + b * p.gb + h * p.gh;
   // a chunk of a tensor on its way to LDS; places behind the last token repeat it
   struct Stage {
@@ -332,8 +320,28 @@ __global__ __launch_bounds__(64 * linear_waves(D)) __attribute__((amdgpu_waves_p
     if (!STATES) fetch(q, p.q, first, qs_);
     if (wave == NW - 1) fetch_decay(first), weights(first, 0);
     if (tid == 0) odd_at = -1;
-    lds_barrier();
   }
+  if (STATES || !p.slots) {
+    given(STATES ? nullptr : p.state);
+  } else {
+    // the state to start from and what the runs before leave of it, a slot ahead
+    f32x4 next[MT];
+    auto load = [&](int i) {
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) next[mt] = *(const f32x4*)(slots + (int64_t)i * (D * D) + place + 256 * mt);
+    };
+    if (p.state) load(p.segments - 1);
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) S[mt] = p.state ? next[mt] : f32x4{};
+    if (seg) load(0);
+    for (int i = 0; i < seg; ++i) {
+      const float a = decays[i];
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) S[mt] = S[mt] * a + next[mt];
+      if (i + 1 < seg) load(i + 1);
+    }
+  }
+  lds_barrier();
   int turn = 0;
   for (int t0 = first; t0 < past; t0 += C, turn ^= 1) {
     lds_barrier();  // the chunk before is done with LDS
@@ -361,118 +369,105 @@ __global__ __launch_bounds__(64 * linear_waves(D)) __attribute__((amdgpu_waves_p
       if (more && wave == NW - 1) weights(t0 + C, turn ^ 1);
     } else {
       const bool dirty = odd_at == t0;
-      const int heads = ONE ? 1 : p.group;
-      for (int j = 0; j < heads; ++j) {
-        const bool other = j + 1 < heads;
-        // not one for all heads: the parts of S would be held beside it
+      if (more) fetch(q, p.q, t0 + C, qs_);
+      // k_j q_i with its decay: row i to a lane's r, tokens j in its registers
+      for (int u = wave; u < UNITS; u += NW) {
+        const int ks = u >= IT, it = ks ? u - IT + TPK : u;
+        Frag qf[STEPS];
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) asm volatile("" : "+v"(S[mt]));
-        if (other) fetch(q + (j + 1) * p.q.sh, p.q, t0, qs_);
-        else if (more) fetch(q, p.q, t0 + C, qs_);
-        // k_j q_i with its decay: row i to a lane's r, tokens j in its registers
-        for (int u = wave; u < UNITS; u += NW) {
-          const int ks = u >= IT, it = ks ? u - IT + TPK : u;
-          Frag qf[STEPS];
+        for (int s = 0; s < STEPS; ++s) qf[s] = At::rows(sq, 16 * it + r, s, g);
+        const double ci = sum[turn][16 * it + r];
+        f32x4 w[TPK];
 #pragma unroll
-          for (int s = 0; s < STEPS; ++s) qf[s] = At::rows(sq, 16 * it + r, s, g);
-          const double ci = sum[turn][16 * it + r];
-          f32x4 w[TPK];
+        for (int i = 0; i < TPK; ++i) {
+          const int jt = ks * TPK + i;
+          w[i] = f32x4{};
+          if (jt > it) continue;
 #pragma unroll
-          for (int i = 0; i < TPK; ++i) {
-            const int jt = ks * TPK + i;
-            w[i] = f32x4{};
-            if (jt > it) continue;
+          for (int s = 0; s < STEPS; ++s) w[i] = At::mma(At::rows(sk, 16 * jt + r, s, g), qf[s], w[i]);
 #pragma unroll
-            for (int s = 0; s < STEPS; ++s) w[i] = At::mma(At::rows(sk, 16 * jt + r, s, g), qf[s], w[i]);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int tj = 16 * jt + 4 * g + e;
-              const float f = __builtin_amdgcn_exp2f((float)(ci - sum[turn][tj])) * w[i][e];
-              w[i][e] = tj <= 16 * it + r ? f : 0.0f;
-            }
-          }
-          Frag f[At::PP];
-          At::template parts<At::PP>(w, 1, f);
-#pragma unroll
-          for (int i = 0; i < At::PP; ++i) sp[(u * At::PP + i) * 64 + lane] = f[i];
-        }
-        if (j == 0 && more && wave == NW - 1) weights(t0 + C, turn ^ 1);
-        lds_barrier();
-        f32x4 o[IT] = {};  // channels col0 + 4 g .. + 3 of token 16 it + r
-#pragma unroll
-        for (int s = 0; s < STEPS; ++s) {
-          Frag f[At::PS];
-          At::template parts<At::PS>(&S[s * TPK], 1, f);
-#pragma unroll
-          for (int it = 0; it < IT; ++it) {
-            const Frag a = At::rows(sq, 16 * it + r, s, g);
-#pragma unroll
-            for (int i = 0; i < At::PS; ++i) o[it] = At::mma(f[i], a, o[it]);
+          for (int e = 0; e < 4; ++e) {
+            const int tj = 16 * jt + 4 * g + e;
+            const float f = __builtin_amdgcn_exp2f((float)(ci - sum[turn][tj])) * w[i][e];
+            w[i][e] = tj <= 16 * it + r ? f : 0.0f;
           }
         }
+        Frag f[At::PP];
+        At::template parts<At::PP>(w, 1, f);
 #pragma unroll
-        for (int it = 0; it < IT; ++it) o[it] *= from[turn][16 * it + r];
+        for (int i = 0; i < At::PP; ++i) sp[(u * At::PP + i) * 64 + lane] = f[i];
+      }
+      if (more && wave == NW - 1) weights(t0 + C, turn ^ 1);
+      lds_barrier();
+      f32x4 o[IT] = {};  // channels col0 + 4 g .. + 3 of token 16 it + r
 #pragma unroll
-        for (int ks = 0; ks < KSTEPS; ++ks) {
-          // 0 times a later value that is no number would still be none: where a
-          // row's tokens and later ones share a step, such values are left out and
-          // added below
-          const Frag f = At::values(sv, ks, col0, lane);
-          Frag own = f;
-          if (__builtin_expect(dirty, 0)) own = At::clean(f);
-#pragma unroll
-          for (int it = ks * TPK; it < IT; ++it)
-#pragma unroll
-            for (int i = 0; i < At::PP; ++i)
-              o[it] = At::mma(it < (ks + 1) * TPK ? own : f, sp[(unit(it, ks) * At::PP + i) * 64 + lane], o[it]);
-        }
-        if (__builtin_expect(dirty, 0)) {
-#pragma nounroll
-          for (int t = 0; t < C; ++t) {
-            float val[4];
-            bool any = false;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) val[e] = Elem<T>::load(sv, t * LD + col0 + 4 * g + e), any |= odd_value(val[e]);
-            if (!__any(any)) continue;
-            // of part 0, row r, token t
-            const int at = 16 / (int)sizeof(T) * (16 * ((t & 15) >> 2) + r) + 4 * (t % KS >> 4) + (t & 3);
-#pragma unroll
-            for (int it = 0; it < IT; ++it) {
-              if (it / TPK != t / KS) continue;
-              float w = 0.0f;
-#pragma unroll
-              for (int i = 0; i < At::PP; ++i)
-                w += Elem<T>::load(sp, (unit(it, it / TPK) * At::PP + i) * (1024 / (int)sizeof(T)) + at);
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                if (t <= 16 * it + r && odd_value(val[e])) o[it][e] += w * val[e];
-            }
-          }
-        }
-        T* const out = (T*)p.o.p + b * p.o.sb + ((int64_t)h * p.group + j) * p.o.sh + col0;
-        const uint32_t to = (uint32_t)(r * (int)p.o.st + 4 * g) * sizeof(T);
+      for (int s = 0; s < STEPS; ++s) {
+        Frag f[At::PS];
+        At::template parts<At::PS>(&S[s * TPK], 1, f);
 #pragma unroll
         for (int it = 0; it < IT; ++it) {
-          const int t = t0 + 16 * it;
-          if (t + r >= past) continue;
-          T* const base = out + (int64_t)t * p.o.st;
-          const f32x4 y = o[it] * p.scale;
-          if constexpr (VEC) {
-            char* const at = (char*)base + to;
-            if constexpr (sizeof(T) == 2) *(uint2*)at = make_uint2(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
-            else *(f32x4*)at = y;
-          } else {
+          const Frag a = At::rows(sq, 16 * it + r, s, g);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) Elem<T>::store(base + r * p.o.st + 4 * g, e, y[e]);
-          }
-        }
-        if (other) {
-          lds_barrier();  // this head is done with sq and sp
-          put(qs_, sq);
-          lds_barrier();
+          for (int i = 0; i < At::PS; ++i) o[it] = At::mma(f[i], a, o[it]);
         }
       }
-      if (!more && !(last && p.state_out)) break;  // nobody reads this state
+#pragma unroll
+      for (int it = 0; it < IT; ++it) o[it] *= from[turn][16 * it + r];
+#pragma unroll
+      for (int ks = 0; ks < KSTEPS; ++ks) {
+        // 0 times a later value that is no number would still be none: where a
+        // row's tokens and later ones share a step, such values are left out and
+        // added below
+        const Frag f = At::values(sv, ks, col0, lane);
+        Frag own = f;
+        if (__builtin_expect(dirty, 0)) own = At::clean(f);
+#pragma unroll
+        for (int it = ks * TPK; it < IT; ++it)
+#pragma unroll
+          for (int i = 0; i < At::PP; ++i)
+            o[it] = At::mma(it < (ks + 1) * TPK ? own : f, sp[(unit(it, ks) * At::PP + i) * 64 + lane], o[it]);
+      }
+      if (__builtin_expect(dirty, 0)) {
+#pragma nounroll
+        for (int t = 0; t < C; ++t) {
+          float val[4];
+          bool any = false;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) val[e] = Elem<T>::load(sv, t * LD + col0 + 4 * g + e), any |= odd_value(val[e]);
+          if (!__any(any)) continue;
+          // of part 0, row r, token t
+          const int at = 16 / (int)sizeof(T) * (16 * ((t & 15) >> 2) + r) + 4 * (t % KS >> 4) + (t & 3);
+#pragma unroll
+          for (int it = 0; it < IT; ++it) {
+            if (it / TPK != t / KS) continue;
+            float w = 0.0f;
+#pragma unroll
+            for (int i = 0; i < At::PP; ++i)
+              w += Elem<T>::load(sp, (unit(it, it / TPK) * At::PP + i) * (1024 / (int)sizeof(T)) + at);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (t <= 16 * it + r && odd_value(val[e])) o[it][e] += w * val[e];
+          }
+        }
+      }
+      T* const out = (T*)p.o.p + b * p.o.sb + ((int64_t)h * p.group + j) * p.o.sh + col0;
+      const uint32_t to = (uint32_t)(r * (int)p.o.st + 4 * g) * sizeof(T);
+#pragma unroll
+      for (int it = 0; it < IT; ++it) {
+        const int t = t0 + 16 * it;
+        if (t + r >= past) continue;
+        T* const base = out + (int64_t)t * p.o.st;
+        const f32x4 y = o[it] * p.scale;
+        if constexpr (VEC) {
+          char* const at = (char*)base + to;
+          if constexpr (sizeof(T) == 2) *(uint2*)at = make_uint2(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
+          else *(f32x4*)at = y;
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) Elem<T>::store(base + r * p.o.st + 4 * g, e, y[e]);
+        }
+      }
+      if (!more && !last) break;  // nobody reads this state
     }
 
     const float a = kept[turn];
@@ -494,7 +489,7 @@ __global__ __launch_bounds__(64 * linear_waves(D)) __attribute__((amdgpu_waves_p
   if (STATES) {
     keep_slot(seg);
     if (tid == THREADS - 64) decays[seg] = power_of_two(total);
-  } else if (last && p.state_out) {
+  } else if (last) {
     float* const at = p.state_out + (int64_t)x * D * D + At::channel(0, g) * D + col0 + r;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
@@ -503,15 +498,16 @@ __global__ __launch_bounds__(64 * linear_waves(D)) __attribute__((amdgpu_waves_p
   }
 }
 
-template <typename T, int D, bool VEC, bool ONE>
+template <typename T, int D, bool VEC>
 hipError_t launch(const LinearParams& p, hipStream_t s) {
-  const dim3 grid((uint32_t)(p.batch * p.kv_heads), p.segments), block(64 * linear_waves(D));
-  if (p.segments > 1) {
-    hipLaunchKernelGGL((linear_chunk_kernel<T, D, true, VEC, true>), grid, block, 0, s, p);
+  const uint32_t heads = p.batch * p.kv_heads;
+  const dim3 block(64 * linear_waves(D));
+  if (p.slots) {
+    hipLaunchKernelGGL((linear_chunk_kernel<T, D, true, VEC>), dim3(heads, p.segments), block, 0, s, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL((linear_chunk_kernel<T, D, false, VEC, ONE>), grid, block, 0, s, p);
+  hipLaunchKernelGGL((linear_chunk_kernel<T, D, false, VEC>), dim3(heads, p.segments, p.group), block, 0, s, p);
   return hipGetLastError();
 }
 
@@ -519,8 +515,7 @@ template <typename T, int D>
 hipError_t launch(const LinearParams& p, hipStream_t s) {
   const int64_t most = (int64_t(1) << 31) / 256 - D;  // 64 rows of 4 bytes an element
   const bool vec = p.q.vec && p.k.vec && p.v.vec && p.o.vec && p.q.st < most && p.k.st < most && p.v.st < most && p.o.st < most;
-  if (!vec) return launch<T, D, false, false>(p, s);
-  return p.group == 1 ? launch<T, D, true, true>(p, s) : launch<T, D, true, false>(p, s);
+  return vec ? launch<T, D, true>(p, s) : launch<T, D, false>(p, s);
 }
 
 template <typename T>

@@ -26,14 +26,15 @@ LinearParams plan_linear(const fluid_tokens* qd, const fluid_tokens* kd) {
   // two workgroups to a compute unit, and runs of two chunks or more
   const int chunk = linear_chunk(qd->dtype);
   const int64_t chunks = (int64_t(p.tokens) + chunk - 1) / chunk;
-  const int64_t runs = std::max<int64_t>(1, std::min<int64_t>(512 / heads, chunks / 2));
+  const int64_t runs = std::max<int64_t>(1, std::min<int64_t>(512 / (heads * p.group), chunks / 2));
+  require(p.group < 65536, "q: more than 65535 heads to one of k's");
   const int64_t each = (chunks + runs - 1) / runs;
   p.run = (int32_t)(each * chunk);
   p.segments = (int32_t)((chunks + each - 1) / each);
   return p;
 }
 uint64_t workspace_of(const LinearParams& p, int head_dim) {
-  return p.segments <= 1 ? 0 : uint64_t(p.batch) * p.kv_heads * p.segments * (head_dim * head_dim + 1) * 4;
+  return p.segments <= 1 && (p.segments == 0 || p.group == 1) ? 0 : uint64_t(p.batch) * p.kv_heads * p.segments * (head_dim * head_dim + 1) * 4;
 }
 
 }  // namespace
@@ -87,6 +88,8 @@ fluid_status fluid_linear_attention(float scale, const fluid_tokens* qd, const v
     p.state_out = state_out;
     p.count = count;
     p.scale = scale;
+    // the state to start from is read by others than write the last one
+    p.slots = p.segments > 1 || (p.segments == 1 && p.group > 1 && state != nullptr && state == state_out);
     const uint64_t need = workspace_of(p, qd->head_dim);
     if (need) {
       if (workspace == nullptr || workspace_bytes < need)

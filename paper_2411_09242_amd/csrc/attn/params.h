@@ -91,7 +91,8 @@ struct LinearParams {
   FastDiv div_heads;
   int32_t segments;  // runs of tokens that workgroups of their own take; 0: token after token
   int32_t run;       // tokens of a run, whole chunks
-  float* ws;         // segments > 1: [head][run] states, then what runs keep of one
+  int32_t slots;     // 1: a first launch leaves states in ws
+  float* ws;         // [kv head][run] states, then what runs keep of one
 };
 
 // tokens of a chunk of linear attention
