@@ -436,12 +436,15 @@ def linear_attention(q, k, v, decay, state=None, count=None, scale=None, out=Non
     it are calls that hand the state on.  Returns (out, state_out)."""
     if out is None:
         out = _zeros(q, stream)
-    _check_grad(q, k, v, decay, out, *(t for t in (state, state_out) if t is not None))
     if state_out is None:
         state_out = _new_state(k, stream)
+    if (q.requires_grad or k.requires_grad or v.requires_grad or decay.requires_grad or out.requires_grad
+            or state_out.requires_grad or (state is not None and state.requires_grad)):
+        _check_grad(q, k, v, decay, out, state_out, *(() if state is None else (state,)))
     key = (fluid._lib, q.dtype, q.shape, q.stride(), q.get_device(), k.dtype, k.shape, k.stride(), k.get_device(),
            v.dtype, v.shape, v.stride(), v.get_device(), out.dtype, out.shape, out.stride(), out.get_device(),
-           _form(decay), None if state is None else _form(state), _form(state_out),
+           decay.dtype, decay.shape, decay.stride(), decay.get_device(), None if state is None else _form(state),
+           state_out.dtype, state_out.shape, state_out.stride(), state_out.get_device(),
            None if count is None else _form(count), "linear")
     made = _calls.get(key)
     if made is None:
@@ -508,7 +511,13 @@ class Rotary:
         turns = torch.empty(dim // 2, dtype=torch.int64)
         fluid._check(_lib().fluid_rotary_turns(_addr(self.desc), turns.data_ptr()))
         self.dim = dim
-        self.turns = turns.to(device)
+        self._turns = turns.to(device)
+        # what every call needs: description, turns, GPU
+        self._call = _addr(self.desc), self._turns.data_ptr(), self._turns.get_device()
+
+    @property
+    def turns(self):
+        return self._turns
 
 
 def _rotary_call(turns, q, k, start, positions, count, q_out, k_out):
@@ -550,15 +559,18 @@ def rotary(turns, q, k=None, start=None, positions=None, count=None, inverse=Fal
         q_out = _zeros(q, stream)
     if k is not None and k_out is None:
         k_out = _zeros(k, stream)
-    _check_grad(q, q_out, *(t for t in (k, k_out) if t is not None))
-    key = (fluid._lib, q.dtype, q.shape, q.stride(), q.get_device(), _form(k), q_out.dtype, q_out.shape, q_out.stride(),
-           q_out.get_device(), _form(k_out), _form(start), _form(positions), _form(count),
-           type(turns) is Rotary and turns.turns.get_device(), "rotary")
+    if q.requires_grad or q_out.requires_grad or (k is not None and (k.requires_grad or k_out.requires_grad)):
+        _check_grad(q, q_out, *(() if k is None else (k, k_out)))
+    desc, at, on = turns._call if isinstance(turns, Rotary) else (None, None, None)
+    key = (fluid._lib, q.dtype, q.shape, q.stride(), q.get_device(), q_out.dtype, q_out.shape, q_out.stride(),
+           q_out.get_device(), None if k is None else _form(k), None if k_out is None else _form(k_out),
+           None if start is None else _form(start), None if positions is None else _form(positions),
+           None if count is None else _form(count), on, "rotary")
     made = _calls.get(key)
     if made is None:
         made = _keep(key, _rotary_call(turns, q, k, start, positions, count, q_out, k_out))
     lib, dev, qd, qod, kd, kod, stride, _ = made
-    _launch(lib.fluid_rotate, dev, C.addressof(turns.desc), turns.turns.data_ptr(),
+    _launch(lib.fluid_rotate, dev, desc, at,
             None if start is None else start.data_ptr(), None if positions is None else positions.data_ptr(), stride,
             None if count is None else count.data_ptr(), 1 if inverse else 0, qd, q.data_ptr(), qod, q_out.data_ptr(),
             kd, None if k is None else k.data_ptr(), kod, None if k_out is None else k_out.data_ptr(),

@@ -35,6 +35,7 @@ typedef short v4i16 __attribute__((ext_vector_type(4)));
 typedef short v8i16 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) v4i16 lds_v4i16;
 
 __device__ __forceinline__ bool odd_value(float x) { return !(fabsf(x) <= 3.402823466e38f); }
@@ -51,10 +52,9 @@ __device__ __forceinline__ void split(f32x4 a, f32x4 b, u32x4 out[N]) {
       if (k == N - 1) {
         out[k][i] = pack_bf16(x, y);
       } else {
-        const uint32_t xh = __float_as_uint(x) & 0xffff0000u, yh = __float_as_uint(y) & 0xffff0000u;
-        out[k][i] = (xh >> 16) | yh;
-        x -= __uint_as_float(xh);
-        y -= __uint_as_float(yh);
+        out[k][i] = __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302);  // the upper halves
+        x -= __uint_as_float(__float_as_uint(x) & 0xffff0000u);
+        y -= __uint_as_float(__float_as_uint(y) & 0xffff0000u);
       }
     }
   }
@@ -67,7 +67,7 @@ struct Core;
 
 template <int D>
 struct Core<uint16_t, D> {
-  static constexpr int C = 64, KS = 32, LD = D + 24;  // tokens of a chunk; a row's elements in LDS: 12 banks apart
+  static constexpr int C = 64, KS = 32, LD = D + 16;  // tokens of a chunk; a row's elements in LDS: 8 banks apart (12: 42 % of its cycles were conflicts)
   static constexpr int PS = 2, PP = 2, PV = 3;       // parts of S, of the weighted products, of v
   typedef u32x4 Frag;
   __device__ static __forceinline__ f32x4 mma(Frag a, Frag b, f32x4 c) {
@@ -116,12 +116,15 @@ struct Core<uint16_t, D> {
       v[i] &= ((v[i] & 0x7f80u) == 0x7f80u ? 0u : 0xffffu) | ((v[i] & 0x7f800000u) == 0x7f800000u ? 0u : 0xffff0000u);
     return v;
   }
-  __device__ static __forceinline__ bool odd(u32x4 v) {
-    bool any = false;
+  // the largest size of a piece's values, as bits, in either half; whether one is no number
+  __device__ static __forceinline__ uint32_t sizes(u32x4 v, uint32_t most) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) any |= (v[i] & 0x7f80u) == 0x7f80u | (v[i] & 0x7f800000u) == 0x7f800000u;
-    return any;
+    for (int i = 0; i < 4; ++i)
+      most = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, v[i] & 0x7fff7fffu),
+                                                                    __builtin_bit_cast(u16x2, most)));
+    return most;
   }
+  __device__ static __forceinline__ bool odd(uint32_t most) { return most >= 0x7f800000u || (most & 0xffffu) >= 0x7f80u; }
 };
 
 template <int D>
@@ -154,12 +157,12 @@ struct Core<float, D> {
     for (int i = 0; i < 4; ++i) v[i] = odd_value(v[i]) ? 0.0f : v[i];
     return v;
   }
-  __device__ static __forceinline__ bool odd(u32x4 v) {
-    bool any = false;
+  __device__ static __forceinline__ uint32_t sizes(u32x4 v, uint32_t most) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) any |= (v[i] & 0x7f800000u) == 0x7f800000u;
-    return any;
+    for (int i = 0; i < 4; ++i) most = max(most, v[i] & 0x7fffffffu);
+    return most;
   }
+  __device__ static __forceinline__ bool odd(uint32_t most) { return most >= 0x7f800000u; }
 };
 
 // 2^c, with what fp32 cuts off of c: what a chunk keeps of a state is used as
@@ -219,7 +222,7 @@ __global__ __launch_bounds__(64 * linear_waves(D)) __attribute__((amdgpu_waves_p
   auto unit = [](int it, int ks) { return ks ? IT + it - TPK : it; };
   __shared__ __attribute__((aligned(16))) T sk[C * LD], sv[C * LD], sq[STATES ? 8 : C * LD];
   __shared__ Frag sp[STATES ? 1 : UNITS * At::PP * 64];
-  // of this and the next chunk in turn: c_i in powers of two, 2^{c_i}, 2^{c_C - c_i}, 2^{c_C}
+  // of this and the next chunk in turn: c_i in powers of two, scale 2^{c_i}, 2^{c_C - c_i}, 2^{c_C}
   __shared__ __attribute__((aligned(16))) double sum[2][C];
   __shared__ __attribute__((aligned(16))) float from[2][C], to[2][C];
   __shared__ float kept[2];
@@ -306,7 +309,7 @@ __global__ __launch_bounds__(64 * linear_waves(D)) __attribute__((amdgpu_waves_p
     if (STATES) total += all;
     if (lane < C) {
       sum[turn][lane] = c;
-      from[turn][lane] = __builtin_amdgcn_exp2f((float)c);
+      from[turn][lane] = p.scale * __builtin_amdgcn_exp2f((float)c);
       to[turn][lane] = __builtin_amdgcn_exp2f((float)(all - c));
     }
     const float a = power_of_two(all);
@@ -354,10 +357,10 @@ __global__ __launch_bounds__(64 * linear_waves(D)) __attribute__((amdgpu_waves_p
     put(vs_, sv);
     if constexpr (!STATES) {
       put(qs_, sq);
-      bool odd = false;
+      uint32_t most = 0;
 #pragma unroll
-      for (int i = 0; i < PIECES; ++i) odd |= At::odd(vs_.piece[i]);
-      if (odd) odd_at = t0;
+      for (int i = 0; i < PIECES; ++i) most = At::sizes(vs_.piece[i], most);
+      if (At::odd(most)) odd_at = t0;
     }
     lds_barrier();
     const bool more = t0 + C < past;
@@ -388,8 +391,8 @@ __global__ __launch_bounds__(64 * linear_waves(D)) __attribute__((amdgpu_waves_p
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const int tj = 16 * jt + 4 * g + e;
-            const float f = __builtin_amdgcn_exp2f((float)(ci - sum[turn][tj])) * w[i][e];
-            w[i][e] = tj <= 16 * it + r ? f : 0.0f;
+            const float f = __builtin_amdgcn_exp2f((float)(ci - sum[turn][tj])) * p.scale;
+            w[i][e] = tj <= 16 * it + r ? f * w[i][e] : 0.0f;
           }
         }
         Frag f[At::PP];
@@ -457,7 +460,7 @@ __global__ __launch_bounds__(64 * linear_waves(D)) __attribute__((amdgpu_waves_p
         const int t = t0 + 16 * it;
         if (t + r >= past) continue;
         T* const base = out + (int64_t)t * p.o.st;
-        const f32x4 y = o[it] * p.scale;
+        const f32x4 y = o[it];
         if constexpr (VEC) {
           char* const at = (char*)base + to;
           if constexpr (sizeof(T) == 2) *(uint2*)at = make_uint2(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));

@@ -76,8 +76,14 @@ class W4:
         n = w4_bytes(rows, cols, group)
         if packed.dtype != _torch().uint8 or packed.dim() != 1 or packed.numel() != n or not packed.is_contiguous():
             _refuse(f"packed: {n} contiguous bytes are needed for [{rows}, {cols}] in groups of {group}")
-        self.packed, self.rows, self.cols, self.group = packed, rows, cols, group
+        self._packed, self.rows, self.cols, self.group = packed, rows, cols, group
         self.desc = _desc(rows, cols, group)
+        # what every call needs: description, bytes, and what they look like
+        self._call = _addr(self.desc), packed.data_ptr(), (rows, cols, group, packed.get_device())
+
+    @property
+    def packed(self):
+        return self._packed
 
 
 def _matrix(t, name, device):
@@ -200,17 +206,21 @@ def w4_matmul(x, w, gate=None, add=None, out=None, workspace=None, stream=None):
     if out is None and isinstance(w, W4):
         dtype, shape = x.dtype, tuple(x.shape[:-1]) + (w.rows,)
         out = _on(stream if x.is_cuda else None, x.get_device(), lambda: _torch().empty(shape, dtype=dtype, device=x.device))
-    _check_grad(x, *(t for t in (add, out) if t is not None))
-    key = (fluid._lib, x.dtype, x.shape, x.stride(), x.get_device(), _form(add), _form(out),
-           isinstance(w, W4) and (w.rows, w.cols, w.group, w.packed.get_device()),
-           isinstance(gate, W4) and (gate.rows, gate.cols, gate.group, gate.packed.get_device()), gate is None, "w4")
+    if x.requires_grad or (out is not None and out.requires_grad) or (add is not None and add.requires_grad):
+        _check_grad(x, *(t for t in (add, out) if t is not None))
+    desc, packed, form = w._call if isinstance(w, W4) else (None, None, None)
+    if gate is None:
+        gated = gate_form = None
+    else:
+        _, gated, gate_form = gate._call if isinstance(gate, W4) else (None, None, False)
+    key = (fluid._lib, x.dtype, x.shape, x.stride(), x.get_device(), None if add is None else _form(add),
+           None if out is None else _form(out), form, gate_form, "w4")
     made = _calls.get(key)
     if made is None:
         made = _keep(key, _matmul_call(x, w, gate, add, out))
     lib, dev, xd, ad, od, need, _ = made
     keep, ws, ws_bytes = _workspace(need, workspace, dev, stream) if need else (None, None, 0)
-    _launch(lib.fluid_w4_matmul, dev, C.addressof(w.desc), w.packed.data_ptr(),
-            None if gate is None else gate.packed.data_ptr(), xd, x.data_ptr(), ad, None if add is None else add.data_ptr(),
+    _launch(lib.fluid_w4_matmul, dev, desc, packed, gated, xd, x.data_ptr(), ad, None if add is None else add.data_ptr(),
             od, out.data_ptr(), ws, ws_bytes, _raw_stream(dev) if stream is None else _stream(stream, dev))
     if stream is not None:
         _record(stream, dev, x, add, out, w.packed, None if gate is None else gate.packed, workspace)
