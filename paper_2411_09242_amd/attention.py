@@ -511,13 +511,7 @@ class Rotary:
         turns = torch.empty(dim // 2, dtype=torch.int64)
         fluid._check(_lib().fluid_rotary_turns(_addr(self.desc), turns.data_ptr()))
         self.dim = dim
-        self._turns = turns.to(device)
-        # what every call needs: description, turns, GPU
-        self._call = _addr(self.desc), self._turns.data_ptr(), self._turns.get_device()
-
-    @property
-    def turns(self):
-        return self._turns
+        self.turns = turns.to(device)
 
 
 def _rotary_call(turns, q, k, start, positions, count, q_out, k_out):
@@ -561,7 +555,7 @@ def rotary(turns, q, k=None, start=None, positions=None, count=None, inverse=Fal
         k_out = _zeros(k, stream)
     if q.requires_grad or q_out.requires_grad or (k is not None and (k.requires_grad or k_out.requires_grad)):
         _check_grad(q, q_out, *(() if k is None else (k, k_out)))
-    desc, at, on = turns._call if isinstance(turns, Rotary) else (None, None, None)
+    on = turns.turns.get_device() if isinstance(turns, Rotary) else None
     key = (fluid._lib, q.dtype, q.shape, q.stride(), q.get_device(), q_out.dtype, q_out.shape, q_out.stride(),
            q_out.get_device(), None if k is None else _form(k), None if k_out is None else _form(k_out),
            None if start is None else _form(start), None if positions is None else _form(positions),
@@ -570,7 +564,7 @@ def rotary(turns, q, k=None, start=None, positions=None, count=None, inverse=Fal
     if made is None:
         made = _keep(key, _rotary_call(turns, q, k, start, positions, count, q_out, k_out))
     lib, dev, qd, qod, kd, kod, stride, _ = made
-    _launch(lib.fluid_rotate, dev, desc, at,
+    _launch(lib.fluid_rotate, dev, C.addressof(turns.desc), turns.turns.data_ptr(),
             None if start is None else start.data_ptr(), None if positions is None else positions.data_ptr(), stride,
             None if count is None else count.data_ptr(), 1 if inverse else 0, qd, q.data_ptr(), qod, q_out.data_ptr(),
             kd, None if k is None else k.data_ptr(), kod, None if k_out is None else k_out.data_ptr(),

@@ -76,14 +76,8 @@ class W4:
         n = w4_bytes(rows, cols, group)
         if packed.dtype != _torch().uint8 or packed.dim() != 1 or packed.numel() != n or not packed.is_contiguous():
             _refuse(f"packed: {n} contiguous bytes are needed for [{rows}, {cols}] in groups of {group}")
-        self._packed, self.rows, self.cols, self.group = packed, rows, cols, group
+        self.packed, self.rows, self.cols, self.group = packed, rows, cols, group
         self.desc = _desc(rows, cols, group)
-        # what every call needs: description, bytes, and what they look like
-        self._call = _addr(self.desc), packed.data_ptr(), (rows, cols, group, packed.get_device())
-
-    @property
-    def packed(self):
-        return self._packed
 
 
 def _matrix(t, name, device):
@@ -117,6 +111,10 @@ def _check_w4(w, name, device):
         _refuse(f"{name}: a W4 is needed")
     if w.packed.get_device() != device:
         _refuse(f"{name}: on {w.packed.device}, not on GPU {device}")
+
+
+def _w4_form(w):
+    return (w.rows, w.cols, w.group, w.packed.get_device()) if isinstance(w, W4) else False
 
 
 def _on(stream, device, make):
@@ -208,19 +206,15 @@ def w4_matmul(x, w, gate=None, add=None, out=None, workspace=None, stream=None):
         out = _on(stream if x.is_cuda else None, x.get_device(), lambda: _torch().empty(shape, dtype=dtype, device=x.device))
     if x.requires_grad or (out is not None and out.requires_grad) or (add is not None and add.requires_grad):
         _check_grad(x, *(t for t in (add, out) if t is not None))
-    desc, packed, form = w._call if isinstance(w, W4) else (None, None, None)
-    if gate is None:
-        gated = gate_form = None
-    else:
-        _, gated, gate_form = gate._call if isinstance(gate, W4) else (None, None, False)
     key = (fluid._lib, x.dtype, x.shape, x.stride(), x.get_device(), None if add is None else _form(add),
-           None if out is None else _form(out), form, gate_form, "w4")
+           None if out is None else _form(out), _w4_form(w), None if gate is None else _w4_form(gate), "w4")
     made = _calls.get(key)
     if made is None:
         made = _keep(key, _matmul_call(x, w, gate, add, out))
     lib, dev, xd, ad, od, need, _ = made
     keep, ws, ws_bytes = _workspace(need, workspace, dev, stream) if need else (None, None, 0)
-    _launch(lib.fluid_w4_matmul, dev, desc, packed, gated, xd, x.data_ptr(), ad, None if add is None else add.data_ptr(),
+    _launch(lib.fluid_w4_matmul, dev, C.addressof(w.desc), w.packed.data_ptr(),
+            None if gate is None else gate.packed.data_ptr(), xd, x.data_ptr(), ad, None if add is None else add.data_ptr(),
             od, out.data_ptr(), ws, ws_bytes, _raw_stream(dev) if stream is None else _stream(stream, dev))
     if stream is not None:
         _record(stream, dev, x, add, out, w.packed, None if gate is None else gate.packed, workspace)
