@@ -24,6 +24,8 @@
 // bf16: S and the weighted products are two bf16 parts (cut off, and the rest
 // rounded: 2^-16), v with its decay three (2^-24): S is as exact as with fp32
 // products.  fp32: the fp32 matrix cores.
+#include <type_traits>
+
 #include "dev_attn.h"
 #include "launch_attn.h"
 
@@ -345,10 +347,12 @@ __global__ __launch_bounds__(64 * linear_waves(D)) __attribute__((amdgpu_waves_p
     }
   }
   lds_barrier();
-  int turn = 0;
-  for (int t0 = first; t0 < past; t0 += C, turn ^= 1) {
+  // A chunk; the last one apart, so that the others have no branch with loads or
+  // stores in it, behind which the compiler would wait for all of them.
+  auto chunk = [&](int t0, int turn, auto last_one) {
+    constexpr bool more = !decltype(last_one)::value;
     lds_barrier();  // the chunk before is done with LDS
-    if (past - t0 < C) {  // nothing from behind the last token enters the state
+    if (!more && past - t0 < C) {  // nothing from behind the last token enters the state
 #pragma unroll
       for (int i = 0; i < PIECES; ++i)
         if (row + ROWS * i >= past - t0) vs_.piece[i] = u32x4{};
@@ -363,16 +367,15 @@ __global__ __launch_bounds__(64 * linear_waves(D)) __attribute__((amdgpu_waves_p
       if (At::odd(most)) odd_at = t0;
     }
     lds_barrier();
-    const bool more = t0 + C < past;
-    if (more) {
+    if constexpr (more) {
       fetch(k, p.k, t0 + C, ks_);
       fetch(v, p.v, t0 + C, vs_);
+      if constexpr (!STATES) fetch(q, p.q, t0 + C, qs_);
     }
     if constexpr (STATES) {
       if (more && wave == NW - 1) weights(t0 + C, turn ^ 1);
     } else {
       const bool dirty = odd_at == t0;
-      if (more) fetch(q, p.q, t0 + C, qs_);
       // k_j q_i with its decay: row i to a lane's r, tokens j in its registers
       for (int u = wave; u < UNITS; u += NW) {
         const int ks = u >= IT, it = ks ? u - IT + TPK : u;
@@ -458,7 +461,7 @@ __global__ __launch_bounds__(64 * linear_waves(D)) __attribute__((amdgpu_waves_p
 #pragma unroll
       for (int it = 0; it < IT; ++it) {
         const int t = t0 + 16 * it;
-        if (t + r >= past) continue;
+        if (!more && t + r >= past) continue;
         T* const base = out + (int64_t)t * p.o.st;
         const f32x4 y = o[it];
         if constexpr (VEC) {
@@ -470,7 +473,7 @@ __global__ __launch_bounds__(64 * linear_waves(D)) __attribute__((amdgpu_waves_p
           for (int e = 0; e < 4; ++e) Elem<T>::store(base + r * p.o.st + 4 * g, e, y[e]);
         }
       }
-      if (!more && !last) break;  // nobody reads this state
+      if (!more && !last) return;  // nobody reads this state
     }
 
     const float a = kept[turn];
@@ -488,7 +491,10 @@ __global__ __launch_bounds__(64 * linear_waves(D)) __attribute__((amdgpu_waves_p
         for (int i = 0; i < At::PV; ++i) S[mt] = At::mma(kt, f[i], S[mt]);
       }
     }
-  }
+  };
+  int t0 = first, turn = 0;
+  for (; t0 + C < past; t0 += C, turn ^= 1) chunk(t0, turn, std::false_type());
+  if (t0 < past) chunk(t0, turn, std::true_type());
   if (STATES) {
     keep_slot(seg);
     if (tid == THREADS - 64) decays[seg] = power_of_two(total);

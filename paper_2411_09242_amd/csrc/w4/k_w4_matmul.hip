@@ -10,14 +10,17 @@ namespace fluid {
 
 namespace {
 
-// NT: tiles of 16 rows of the matrix.
-template <typename T, int G, int NT, bool GATE>
+// NT: tiles of 16 rows of the matrix.  VEC: eight channels of a row of x are 16-byte
+// loads.
+template <typename T, int G, int NT, bool GATE, bool VEC>
 __global__ __launch_bounds__(GATE || NT == 2 || sizeof(T) == 4 ? 512 : 1024) void w4_few_kernel(W4Params p) {
   constexpr int MATS = GATE ? 2 : 1, GROUPS = 128 / G, STEPS = G / 32, P = Rows<T>::N;
   extern __shared__ float sums[];  // [wavefront][matrix][tile][256]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
   const int tile0 = blockIdx.x * NT;
   const u32x4 ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
+
+  const int row = min(r, p.m - 1);  // those behind the last are not stored
 
   // a block of 128 channels of the matrices and of x
   struct Block {
@@ -36,20 +39,22 @@ __global__ __launch_bounds__(GATE || NT == 2 || sizeof(T) == 4 ? 512 : 1024) voi
         const uint8_t* const pairs = of.pairs + at * (64 * GROUPS) + r * (4 * GROUPS);
         load_pairs<GROUPS>(pairs, to.sb[a][i]);
       }
-    const bool whole = p.vec && 128 * c + 128 <= p.k;
-    const T* const x = (const T*)p.x + r * p.xs + 128 * c + 8 * g;
+    const T* const x = (const T*)p.x + row * p.xs;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      to.x[j].clear();
-      if (r < p.m) {
-        if (whole) to.x[j].load(x + 32 * j);
-        else to.x[j].load(x + 32 * j, p.k - (128 * c + 32 * j + 8 * g));
-      }
+      const int ch = 128 * c + 32 * j + 8 * g;
+      if constexpr (VEC) to.x[j].load(x + min(ch, p.k - 8));
+      else to.x[j].load(x + ch, p.k - ch);
     }
   };
 
   f32x4 y[MATS][NT] = {};
-  auto multiply = [&](const Block& in) {
+  auto multiply = [&](int c, Block& in) {
+    if (VEC && 128 * c + 128 > p.k) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (128 * c + 32 * j + 8 * g >= p.k) in.x[j].clear();
+    }
 #pragma unroll
     for (int i = 0; i < GROUPS; ++i) {
       f32x4 part[MATS][NT] = {}, all = {};
@@ -74,16 +79,21 @@ __global__ __launch_bounds__(GATE || NT == 2 || sizeof(T) == 4 ? 512 : 1024) voi
         for (int u = 0; u < NT; ++u) add_group<T>(in.sb[a][u][i], part[a][u], all, y[a][u]);
     }
   };
-  // the next block is on its way while one is multiplied
+  // The next block is on its way while one is multiplied.  The last one is loaded
+  // twice rather than not: behind a branch that may have loads or not, the compiler
+  // waits for all of them.
   Block one, two;
+  const int last = p.blocks - 1;
   int c = wave;
-  if (c < p.blocks) fetch(c, one);
-  for (; c < p.blocks; c += 2 * p.waves) {
-    if (c + p.waves < p.blocks) fetch(c + p.waves, two);
-    multiply(one);
-    if (c + p.waves >= p.blocks) break;
-    if (c + 2 * p.waves < p.blocks) fetch(c + 2 * p.waves, one);
-    multiply(two);
+  fetch(min(c, last), one);
+  while (c <= last) {
+    fetch(min(c + p.waves, last), two);
+    multiply(c, one);
+    c += p.waves;
+    if (c > last) break;
+    fetch(min(c + p.waves, last), one);
+    multiply(c, two);
+    c += p.waves;
   }
 #pragma unroll
   for (int a = 0; a < MATS; ++a)
@@ -107,12 +117,16 @@ __global__ __launch_bounds__(GATE || NT == 2 || sizeof(T) == 4 ? 512 : 1024) voi
 template <typename T, int G, int NT, bool GATE>
 hipError_t launch(const W4Params& p, hipStream_t s) {
   const dim3 grid((p.tiles + NT - 1) / NT), block(64 * p.waves);
-  hipLaunchKernelGGL((w4_few_kernel<T, G, NT, GATE>), grid, block, p.waves * (GATE ? 2 : 1) * NT * 1024, s, p);
+  const int lds = p.waves * (GATE ? 2 : 1) * NT * 1024;
+  if (p.vec) hipLaunchKernelGGL((w4_few_kernel<T, G, NT, GATE, true>), grid, block, lds, s, p);
+  else hipLaunchKernelGGL((w4_few_kernel<T, G, NT, GATE, false>), grid, block, lds, s, p);
   return hipGetLastError();
 }
 template <typename T, int G, bool GATE>
 hipError_t launch_rows(const W4Params& p, hipStream_t s) {
-  return p.wide ? launch<T, G, 2, GATE>(p, s) : launch<T, G, 1, GATE>(p, s);
+  if constexpr (!GATE)
+    if (p.wide) return launch<T, G, 2, GATE>(p, s);
+  return launch<T, G, 1, GATE>(p, s);
 }
 template <typename T>
 hipError_t launch_group(const W4Params& p, hipStream_t s) {

@@ -22,11 +22,12 @@ __device__ __forceinline__ void lds_barrier() {
   asm volatile("" ::: "memory");
 }
 
-// MT: tiles of 16 rows of x.
-template <typename T, int G, int MT, bool GATE>
+// MT: tiles of 16 rows of x.  VEC: eight channels of a row of x are 16-byte loads.
+template <typename T, int G, int MT, bool GATE, bool VEC>
 __global__ __launch_bounds__(64 * kWaves) void w4_rows_kernel(W4Params p) {
   constexpr int MATS = GATE ? 2 : 1, GROUPS = 128 / G, STEPS = G / 32, P = Rows<T>::N;
-  constexpr int PIECES = MT * 4 * 64 / (64 * kWaves) > 0 ? MT * 4 * 64 / (64 * kWaves) : 1;  // of x, of a thread
+  constexpr int PIECES = MT * 4 / kWaves;  // of x, of a thread
+  static_assert(PIECES * kWaves == MT * 4, "whole pieces");
   __shared__ u32x4 sx[2][4 * MT * P * 64];  // [step][tile][part][lane]
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
   const int tile = blockIdx.x * kWaves + wave, m0 = blockIdx.z * (16 * MT);
@@ -46,29 +47,28 @@ __global__ __launch_bounds__(64 * kWaves) void w4_rows_kernel(W4Params p) {
       load_pairs<GROUPS>(of.pairs + at * (64 * GROUPS) + r * (4 * GROUPS), to.sb[a]);
     }
   };
-  // thread i's pieces: of step and tile wave + kWaves i, lane's place
+  // a thread's pieces: of step and tile wave + kWaves i, lane's place
+  auto channel = [&](int c, int i) { return 128 * c + 32 * ((wave + kWaves * i) / MT) + 8 * g; };
   auto fetch_x = [&](int c, Rows<T> to[PIECES]) {
-    const bool whole = p.vec && 128 * c + 128 <= p.k;
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
-      const int u = wave + kWaves * i, row = m0 + 16 * (u % MT) + r, ch = 128 * c + 32 * (u / MT) + 8 * g;
-      to[i].clear();
-      if (u < 4 * MT && row < p.m) {
-        const T* const x = (const T*)p.x + row * p.xs + ch;
-        if (whole) to[i].load(x);
-        else to[i].load(x, p.k - ch);
-      }
+      // rows behind the last are not stored, channels behind the last cleared below
+      const int row = min(m0 + 16 * ((wave + kWaves * i) % MT) + r, p.m - 1), ch = channel(c, i);
+      const T* const x = (const T*)p.x + row * p.xs;
+      if constexpr (VEC) to[i].load(x + min(ch, p.k - 8));
+      else to[i].load(x + ch, p.k - ch);
     }
   };
-  auto put = [&](const Rows<T> from[PIECES], u32x4* to) {
+  auto put = [&](int c, Rows<T> from[PIECES], u32x4* to) {
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
       const int u = wave + kWaves * i;
+      if (VEC && 128 * c + 128 > p.k && channel(c, i) >= p.k) from[i].clear();
       u32x4 part[P];
       from[i].parts(part);
 #pragma unroll
       for (int k = 0; k < P; ++k)
-        if (u < 4 * MT) to[(u * P + k) * 64 + lane] = part[k];
+        to[(u * P + k) * 64 + lane] = part[k];
     }
   };
 
@@ -99,26 +99,27 @@ __global__ __launch_bounds__(64 * kWaves) void w4_rows_kernel(W4Params p) {
     }
   };
 
-  // words are on their way four blocks ahead (of HBM, some 1.5 us; a block takes
-  // 0.4), x's three: two in registers, one in LDS
+  // Words are on their way four blocks ahead, x three: two in registers, one in LDS.
+  // The last block is loaded again rather than nothing: behind a branch that may
+  // have loads or not, the compiler waits for all of them.
   Words words[4];
   Rows<T> xr[2][PIECES];
+  const int last = past - 1;
   fetch_x(first, xr[0]);
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (first + i < past) fetch_words(first + i, words[i]);
-  put(xr[0], sx[0]);
-  if (first + 1 < past) fetch_x(first + 1, xr[1]);
-  if (first + 2 < past) fetch_x(first + 2, xr[0]);
+  for (int i = 0; i < 4; ++i) fetch_words(min(first + i, last), words[i]);
+  fetch_x(min(first + 1, last), xr[1]);
+  put(first, xr[0], sx[0]);
+  fetch_x(min(first + 2, last), xr[0]);
   lds_barrier();
   for (int c = first; c < past; c += 4) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       if (c + i >= past) break;
-      if (c + i + 1 < past) put(xr[(i + 1) % 2], sx[(i + 1) % 2]);
-      if (c + i + 3 < past) fetch_x(c + i + 3, xr[(i + 1) % 2]);
+      put(min(c + i + 1, last), xr[(i + 1) % 2], sx[(i + 1) % 2]);
+      fetch_x(min(c + i + 3, last), xr[(i + 1) % 2]);
       multiply(words[i], sx[i % 2]);
-      if (c + i + 4 < past) fetch_words(c + i + 4, words[i]);
+      fetch_words(min(c + i + 4, last), words[i]);
       lds_barrier();
     }
   }
@@ -157,7 +158,8 @@ __global__ __launch_bounds__(256) void w4_join_kernel(W4Params p) {
 template <typename T, int G, int MT, bool GATE>
 hipError_t launch(const W4Params& p, hipStream_t s) {
   const dim3 grid((p.tiles + kWaves - 1) / kWaves, p.splits, (p.m + 16 * MT - 1) / (16 * MT)), block(64 * kWaves);
-  hipLaunchKernelGGL((w4_rows_kernel<T, G, MT, GATE>), grid, block, 0, s, p);
+  if (p.vec) hipLaunchKernelGGL((w4_rows_kernel<T, G, MT, GATE, true>), grid, block, 0, s, p);
+  else hipLaunchKernelGGL((w4_rows_kernel<T, G, MT, GATE, false>), grid, block, 0, s, p);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
   hipLaunchKernelGGL((w4_join_kernel<T, GATE>), dim3((p.n + 255) / 256, p.m), dim3(256), 0, s, p);
@@ -166,7 +168,6 @@ hipError_t launch(const W4Params& p, hipStream_t s) {
 template <typename T, int G>
 hipError_t launch_rows(const W4Params& p, hipStream_t s) {
   const bool gate = p.gate.words != nullptr;
-  if (p.m <= 16) return gate ? launch<T, G, 1, true>(p, s) : launch<T, G, 1, false>(p, s);
   if (p.m <= 32) return gate ? launch<T, G, 2, true>(p, s) : launch<T, G, 2, false>(p, s);
   return gate ? launch<T, G, 4, true>(p, s) : launch<T, G, 4, false>(p, s);
 }
