@@ -320,32 +320,35 @@ __global__ __launch_bounds__(64 * linear_waves(D)) __attribute__((amdgpu_waves_p
 
   Stage ks_, vs_, qs_;
   if (first < past) {
+    if (wave == NW - 1) fetch_decay(first);  // ahead of what all workgroups ask for now
     fetch(k, p.k, first, ks_);
     fetch(v, p.v, first, vs_);
     if (!STATES) fetch(q, p.q, first, qs_);
-    if (wave == NW - 1) fetch_decay(first), weights(first, 0);
     if (tid == 0) odd_at = -1;
   }
   if (STATES || !p.slots) {
     given(STATES ? nullptr : p.state);
   } else {
-    // the state to start from and what the runs before leave of it, a slot ahead
+    // the state to start from and what the runs before leave of it, a slot ahead;
+    // after the scan, this run's own
     f32x4 next[MT];
     auto load = [&](int i) {
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) next[mt] = *(const f32x4*)(slots + (int64_t)i * (D * D) + place + 256 * mt);
     };
-    if (p.state) load(p.segments - 1);
+    if (p.state || p.scan) load(p.scan ? seg : p.segments - 1);
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) S[mt] = p.state ? next[mt] : f32x4{};
-    if (seg) load(0);
-    for (int i = 0; i < seg; ++i) {
+    for (int mt = 0; mt < MT; ++mt) S[mt] = p.state || p.scan ? next[mt] : f32x4{};
+    const int before = p.scan ? 0 : seg;
+    if (before) load(0);
+    for (int i = 0; i < before; ++i) {
       const float a = decays[i];
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) S[mt] = S[mt] * a + next[mt];
-      if (i + 1 < seg) load(i + 1);
+      if (i + 1 < before) load(i + 1);
     }
   }
+  if (first < past && wave == NW - 1) weights(first, 0);
   lds_barrier();
   // A chunk; the last one apart, so that the others have no branch with loads or
   // stores in it, behind which the compiler would wait for all of them.
@@ -386,9 +389,8 @@ __global__ __launch_bounds__(64 * linear_waves(D)) __attribute__((amdgpu_waves_p
         f32x4 w[TPK];
 #pragma unroll
         for (int i = 0; i < TPK; ++i) {
-          const int jt = ks * TPK + i;
+          const int jt = ks * TPK + i;  // past `it` too: all masked
           w[i] = f32x4{};
-          if (jt > it) continue;
 #pragma unroll
           for (int s = 0; s < STEPS; ++s) w[i] = At::mma(At::rows(sk, 16 * jt + r, s, g), qf[s], w[i]);
 #pragma unroll
@@ -507,14 +509,45 @@ __global__ __launch_bounds__(64 * linear_waves(D)) __attribute__((amdgpu_waves_p
   }
 }
 
+// What runs add to a state into what each starts from, in place: a thread has four
+// values of a head's state.
+__global__ __launch_bounds__(256) void linear_scan_kernel(LinearParams p, int size) {
+  constexpr int AHEAD = 8;
+  const int x = blockIdx.y, at = (blockIdx.x * 256 + threadIdx.x) * 4;
+  float* const slots = p.ws + (int64_t)x * p.segments * size + at;
+  const float* const decays = p.ws + (int64_t)gridDim.y * p.segments * size + (int64_t)x * p.segments;
+  const int last = p.segments - 1;
+  f32x4 S = p.state ? *(const f32x4*)(slots + (int64_t)last * size) : f32x4{};
+  for (int i = 0; i <= last; i += AHEAD) {
+    f32x4 u[AHEAD];
+    float a[AHEAD];
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) {
+      u[j] = *(const f32x4*)(slots + (int64_t)min(i + j, last) * size);
+      a[j] = decays[min(i + j, last)];
+    }
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j)
+      if (i + j <= last) {
+        *(f32x4*)(slots + (int64_t)(i + j) * size) = S;
+        S = S * a[j] + u[j];
+      }
+  }
+}
+
 template <typename T, int D, bool VEC>
 hipError_t launch(const LinearParams& p, hipStream_t s) {
   const uint32_t heads = p.batch * p.kv_heads;
   const dim3 block(64 * linear_waves(D));
   if (p.slots) {
     hipLaunchKernelGGL((linear_chunk_kernel<T, D, true, VEC>), dim3(heads, p.segments), block, 0, s, p);
-    const hipError_t e = hipGetLastError();
+    hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
+    if (p.scan) {
+      hipLaunchKernelGGL(linear_scan_kernel, dim3(D * D / 1024, heads), dim3(256), 0, s, p, D * D);
+      e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
   }
   hipLaunchKernelGGL((linear_chunk_kernel<T, D, false, VEC>), dim3(heads, p.segments, p.group), block, 0, s, p);
   return hipGetLastError();

@@ -22,7 +22,7 @@ LinearParams plan_linear(const fluid_tokens* qd, const fluid_tokens* kd) {
   // a workgroup of 256 threads to 32 columns of a state
   const int64_t heads = product({p.batch, p.kv_heads});
   require(product({heads, kd->head_dim / 32, 256}) <= kMostThreads, "q: too large for one launch");
-  if (p.tokens <= 8) return p;
+  if (p.tokens <= 2 || int64_t(p.tokens) * p.group <= 4) return p;
   // two workgroups to a compute unit, and runs of two chunks or more
   const int chunk = linear_chunk(qd->dtype);
   const int64_t chunks = (int64_t(p.tokens) + chunk - 1) / chunk;
@@ -31,6 +31,7 @@ LinearParams plan_linear(const fluid_tokens* qd, const fluid_tokens* kd) {
   const int64_t each = (chunks + runs - 1) / runs;
   p.run = (int32_t)(each * chunk);
   p.segments = (int32_t)((chunks + each - 1) / each);
+  p.scan = p.group * p.segments > 24;
   return p;
 }
 uint64_t workspace_of(const LinearParams& p, int head_dim) {

@@ -92,6 +92,7 @@ struct LinearParams {
   int32_t segments;  // runs of tokens that workgroups of their own take; 0: token after token
   int32_t run;       // tokens of a run, whole chunks
   int32_t slots;     // 1: a first launch leaves states in ws
+  int32_t scan;      // 1: a launch between them makes the runs' first states
   float* ws;         // [kv head][run] states, then what runs keep of one
 };
 

@@ -116,8 +116,8 @@ fluid_status fluid_rotate(const fluid_rotary* r, const uint64_t* turns, const in
     p.pairs = r->interleaved ? r->dim / (p.vec ? wide : 2) : r->dim / 2 / at_once;
     p.units = p.pairs + (p.tail ? (p.head_dim - p.dim) / at_once : 0);
     const int64_t heads = int64_t(p.heads[0]) + p.heads[1], rows = product({p.batch, p.tokens, p.units});
-    // a thread's angles serve up to eight heads where that still fills the GPU
-    const int64_t few = (heads + 7) / 8;
+    // a thread's angles serve up to four heads where that still fills the GPU
+    const int64_t few = (heads + 3) / 4;
     p.head_threads = (int32_t)(product({rows, few}) >= 131072 ? few : heads);
     const int64_t items = product({rows, p.head_threads});
     require(heads < int64_t(1) << 31 && items <= kMostThreads - 255, "q, k: too large for one launch");

@@ -58,8 +58,9 @@ void plan_product(W4Params& p, int32_t rows, bool gate, int dtype) {
   require(int64_t(p.tiles) * 1024 < int64_t(1) << 32, "w: too large for one launch");
   if (rows <= 16) {
     // wavefronts with blocks of their own
-    p.wide = p.tiles >= 1024 && !gate;
-    p.waves = p.blocks >= 16 && !gate && !p.wide && dtype == FLUID_BF16 ? 16 : p.blocks >= 8 ? 8 : 4;
+    p.wide = p.tiles >= 512 && !gate;
+    const bool many = gate || p.wide;
+    p.waves = p.blocks < 8 || (many && dtype == FLUID_BF16) ? 4 : p.blocks < 16 || dtype != FLUID_BF16 ? 8 : 16;
     return;
   }
   // as many runs as make a workgroup to a compute unit, of four blocks or more
