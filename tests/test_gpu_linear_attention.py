@@ -149,6 +149,26 @@ def test_state_in_place_and_handed_on(dtype, T):
         check((both, rest[1]), q, k, v, g, state, [T] * B, 0.1, dtype)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [1, 3, 40, 900])
+def test_shared_heads_in_place_and_without_a_state(dtype, T):
+    """Several heads start from a state that one of them overwrites; runs of
+    tokens whose states a launch of its own adds up."""
+    B, H, Hk, D = 2, 12, 2, 64
+    q, k, v = rand(1, B, T, H, D, dtype=dtype), rand(2, B, T, Hk, D, dtype=dtype), rand(3, B, T, Hk, D, dtype=dtype)
+    g, state, counts = decays(4, B, T, Hk, True), rand(5, B, Hk, D, D), [T, max(0, T - 500)]
+    for start in (state, None):
+        apart = torch.full_like(q, 9.0)
+        want = A.linear_attention(q, k, v, g, state=start, count=ints(counts), scale=0.1, out=apart)
+        check(want, q, k, v, g, start, counts, 0.1, dtype)
+    mine, out = state.clone(), torch.full_like(q, 9.0)
+    want = A.linear_attention(q, k, v, g, state=state, count=ints(counts), scale=0.1, out=apart)
+    for _ in range(3):
+        mine.copy_(state)
+        A.linear_attention(q, k, v, g, state=mine, state_out=mine, count=ints(counts), scale=0.1, out=out)
+        assert torch.equal(out, want[0]) and torch.equal(mine, want[1])
+
+
 def test_one_by_one_is_as_all_at_once():
     B, T, H, D = 1, 75, 2, 128
     q, k, v = (rand(i, B, T, H, D, dtype="bf16") for i in (1, 2, 3))
