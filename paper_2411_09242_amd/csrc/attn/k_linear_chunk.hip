@@ -296,6 +296,31 @@ __global__ __launch_bounds__(64 * linear_waves(D)) __attribute__((amdgpu_waves_p
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) *(u32x4*)(s + (row + ROWS * i) * LD + piece) = from.piece[i];
   };
+  // The results of a chunk, which lie where q did, to memory: whole rows, where a
+  // wavefront's own columns would be 32 bytes of each.
+  T* const out = (T*)p.o.p + b * p.o.sb + ((int64_t)h * p.group + j) * p.o.sh;
+  auto take = [&](Stage& to) {
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) to.piece[i] = *(const u32x4*)(sq + (row + ROWS * i) * LD + piece);
+  };
+  auto give = [&](const Stage& from, int t0, int rows) {
+    T* const base = out + (int64_t)t0 * p.o.st;
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+      const int t = row + ROWS * i;
+      if (t >= rows) continue;
+      if constexpr (VEC) {
+        *(u32x4*)((char*)base + (uint32_t)(t * (int)p.o.st + piece) * sizeof(T)) = from.piece[i];
+      } else {
+        T* const to = base + t * p.o.st + piece;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if constexpr (sizeof(T) == 2) to[2 * e] = (uint16_t)from.piece[i][e], to[2 * e + 1] = (uint16_t)(from.piece[i][e] >> 16);
+          else to[e] = __uint_as_float(from.piece[i][e]);
+        }
+      }
+    }
+  };
   // The last wavefront makes the next chunk's weights from decays that it has
   // loaded a chunk before: the others would wait for them.
   double total = 0.0;  // of the run's log decays
@@ -360,6 +385,8 @@ __global__ __launch_bounds__(64 * linear_waves(D)) __attribute__((amdgpu_waves_p
       for (int i = 0; i < PIECES; ++i)
         if (row + ROWS * i >= past - t0) vs_.piece[i] = u32x4{};
     }
+    Stage done;
+    if constexpr (!STATES) take(done);
     put(ks_, sk);
     put(vs_, sv);
     if constexpr (!STATES) {
@@ -370,6 +397,9 @@ __global__ __launch_bounds__(64 * linear_waves(D)) __attribute__((amdgpu_waves_p
       if (At::odd(most)) odd_at = t0;
     }
     lds_barrier();
+    if constexpr (!STATES) {
+      if (t0 != first) give(done, t0 - C, C);
+    }
     if constexpr (more) {
       fetch(k, p.k, t0 + C, ks_);
       fetch(v, p.v, t0 + C, vs_);
@@ -458,22 +488,12 @@ __global__ __launch_bounds__(64 * linear_waves(D)) __attribute__((amdgpu_waves_p
           }
         }
       }
-      T* const out = (T*)p.o.p + b * p.o.sb + ((int64_t)h * p.group + j) * p.o.sh + col0;
-      const uint32_t to = (uint32_t)(r * (int)p.o.st + 4 * g) * sizeof(T);
+      lds_barrier();  // all are done with q: its place takes the result
 #pragma unroll
       for (int it = 0; it < IT; ++it) {
-        const int t = t0 + 16 * it;
-        if (!more && t + r >= past) continue;
-        T* const base = out + (int64_t)t * p.o.st;
-        const f32x4 y = o[it];
-        if constexpr (VEC) {
-          char* const at = (char*)base + to;
-          if constexpr (sizeof(T) == 2) *(uint2*)at = make_uint2(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]));
-          else *(f32x4*)at = y;
-        } else {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) Elem<T>::store(base + r * p.o.st + 4 * g, e, y[e]);
-        }
+        T* const at = sq + (16 * it + r) * LD + col0 + 4 * g;
+        if constexpr (sizeof(T) == 2) *(uint2*)at = make_uint2(pack_bf16(o[it][0], o[it][1]), pack_bf16(o[it][2], o[it][3]));
+        else *(f32x4*)at = o[it];
       }
       if (!more && !last) return;  // nobody reads this state
     }
@@ -496,7 +516,15 @@ __global__ __launch_bounds__(64 * linear_waves(D)) __attribute__((amdgpu_waves_p
   };
   int t0 = first, turn = 0;
   for (; t0 + C < past; t0 += C, turn ^= 1) chunk(t0, turn, std::false_type());
-  if (t0 < past) chunk(t0, turn, std::true_type());
+  if (t0 < past) {
+    chunk(t0, turn, std::true_type());
+    if constexpr (!STATES) {
+      Stage done;
+      lds_barrier();
+      take(done);
+      give(done, t0, past - t0);
+    }
+  }
   if (STATES) {
     keep_slot(seg);
     if (tid == THREADS - 64) decays[seg] = power_of_two(total);
