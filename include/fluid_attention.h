@@ -218,8 +218,9 @@ fluid_status fluid_rotate(const fluid_rotary* r, const uint64_t* turns, const in
  * Arithmetic: fp32 sums and states.  fp32: fp32 products.  bf16: products on the
  * bf16 matrix cores; the state's own are exact to 2^-23, out's factors (q k with
  * its decay, and the state) are two bf16 parts each, 2^-16.  What is not finite in
- * q makes its row not finite, in k and v its and all later rows' and the state,
- * where NaN may stand for an infinity; rows before it stay.  Errors:
+ * q makes its row not finite, in k, v and state its channels of that and all later
+ * rows and of the last state, where NaN may stand for an infinity; rows before it
+ * stay.  Errors:
  * FLUID_E_INVALID; FLUID_E_ARENA_TOO_SMALL (workspace). */
 fluid_status fluid_linear_attention_workspace(const fluid_tokens* qd, const fluid_tokens* kd, uint64_t* bytes);
 fluid_status fluid_linear_attention(float scale, const fluid_tokens* qd, const void* q, const fluid_tokens* kd,

@@ -75,6 +75,24 @@ __device__ __forceinline__ f16x8 word_values(const Magic& mg, uint32_t w, uint32
   return word_values(mg, w, ss, bb);
 }
 
+// Values beyond it are held in 4 bits as it.
+constexpr float kLimit = 16384.0f;
+// f16 of a value that is first rounded to fp32: fused with the operation before
+// it, the conversion rounds once, which gives another pair for one group in
+// some 20000.
+__device__ __forceinline__ _Float16 half_of(float x) {
+  asm volatile("" : "+v"(x));
+  return (_Float16)x;
+}
+
+// Waits for this wavefront's own LDS accesses and for the other wavefronts; loads
+// and stores of memory stay in flight.
+__device__ __forceinline__ void lds_barrier() {
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
 // Eight neighbouring elements; vec: the address is 16-byte aligned.
 template <typename T>
 struct Eight;

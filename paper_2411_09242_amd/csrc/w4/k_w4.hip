@@ -6,14 +6,6 @@ namespace fluid {
 
 namespace {
 
-constexpr float kLimit = 16384.0f;
-
-// f16 of a value that is first rounded to fp32
-__device__ __forceinline__ _Float16 half_of(float x) {
-  asm volatile("" : "+v"(x));
-  return (_Float16)x;
-}
-
 // A workgroup has a tile of 16 rows and 128 channels: thread 16 r + i the
 // channels 8 i .. + 7 of row r, which are one word.
 template <typename T>

@@ -5,6 +5,11 @@
 // its wavefronts, as operands: two blocks in turn, the loads another one ahead.
 // Where that are too few workgroups, runs of channels go to workgroups of their own,
 // whose sums a second launch adds in order.
+//
+// 32 rows times 4096 x 11008: 16.7 us, 12.5 and 4 in the two launches; with x from L2
+// for every 32 rows of the matrix, one launch, 25.  Vector instructions (levels, and
+// sums times s and b) take 4.4 us, the words' first loads and the sums' way to memory
+// most of the rest.  64 rows 23 us.
 #include "launch_w4.h"
 #include "w4_tile.h"
 
@@ -13,14 +18,6 @@ namespace fluid {
 namespace {
 
 constexpr int kWaves = 8;
-
-// Waits for this wavefront's own LDS accesses and for the other wavefronts; loads
-// of memory stay in flight.
-__device__ __forceinline__ void lds_barrier() {
-  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-  __builtin_amdgcn_s_barrier();
-  asm volatile("" ::: "memory");
-}
 
 // MT: tiles of 16 rows of x.  VEC: eight channels of a row of x are 16-byte loads.
 template <typename T, int G, int MT, bool GATE, bool VEC>
