@@ -15,8 +15,8 @@ namespace fluid {
 
 namespace {
 
-// NT: tiles of 16 rows of the matrix.  VEC: eight channels of a row of x are 16-byte
-// loads.
+// NT: tiles of 16 rows of the matrix.  VEC: x has eight channels or more, which are
+// loaded at once; the last ones end with the row.
 template <typename T, int G, int NT, bool GATE, bool VEC>
 __global__ __launch_bounds__(GATE || NT == 2 || sizeof(T) == 4 ? 512 : 1024) void w4_few_kernel(W4Params p) {
   constexpr int MATS = GATE ? 2 : 1, GROUPS = 128 / G, STEPS = G / 32, P = Rows<T>::N;
@@ -57,8 +57,7 @@ __global__ __launch_bounds__(GATE || NT == 2 || sizeof(T) == 4 ? 512 : 1024) voi
   auto multiply = [&](int c, Block& in) {
     if (VEC && 128 * c + 128 > p.k) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (128 * c + 32 * j + 8 * g >= p.k) in.x[j].clear();
+      for (int j = 0; j < 4; ++j) in.x[j].drop(max(128 * c + 32 * j + 8 * g - (p.k - 8), 0));
     }
 #pragma unroll
     for (int i = 0; i < GROUPS; ++i) {
@@ -123,7 +122,7 @@ template <typename T, int G, int NT, bool GATE>
 hipError_t launch(const W4Params& p, hipStream_t s) {
   const dim3 grid((p.tiles + NT - 1) / NT), block(64 * p.waves);
   const int lds = p.waves * (GATE ? 2 : 1) * NT * 1024;
-  if (p.vec) hipLaunchKernelGGL((w4_few_kernel<T, G, NT, GATE, true>), grid, block, lds, s, p);
+  if (p.k >= 8) hipLaunchKernelGGL((w4_few_kernel<T, G, NT, GATE, true>), grid, block, lds, s, p);
   else hipLaunchKernelGGL((w4_few_kernel<T, G, NT, GATE, false>), grid, block, lds, s, p);
   return hipGetLastError();
 }

@@ -19,7 +19,8 @@ namespace {
 
 constexpr int kWaves = 8;
 
-// MT: tiles of 16 rows of x.  VEC: eight channels of a row of x are 16-byte loads.
+// MT: tiles of 16 rows of x.  VEC: x has eight channels or more, which are loaded at
+// once; the last ones end with the row.
 template <typename T, int G, int MT, bool GATE, bool VEC>
 __global__ __launch_bounds__(64 * kWaves) void w4_rows_kernel(W4Params p) {
   constexpr int MATS = GATE ? 2 : 1, GROUPS = 128 / G, STEPS = G / 32, P = Rows<T>::N;
@@ -49,7 +50,7 @@ __global__ __launch_bounds__(64 * kWaves) void w4_rows_kernel(W4Params p) {
   auto fetch_x = [&](int c, Rows<T> to[PIECES]) {
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
-      // rows behind the last are not stored, channels behind the last cleared below
+      // rows behind the last are not stored, channels behind the last dropped below
       const int row = min(m0 + 16 * ((wave + kWaves * i) % MT) + r, p.m - 1), ch = channel(c, i);
       const T* const x = (const T*)p.x + row * p.xs;
       if constexpr (VEC) to[i].load(x + min(ch, p.k - 8));
@@ -60,7 +61,7 @@ __global__ __launch_bounds__(64 * kWaves) void w4_rows_kernel(W4Params p) {
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
       const int u = wave + kWaves * i;
-      if (VEC && 128 * c + 128 > p.k && channel(c, i) >= p.k) from[i].clear();
+      if (VEC && 128 * c + 128 > p.k) from[i].drop(max(channel(c, i) - (p.k - 8), 0));
       u32x4 part[P];
       from[i].parts(part);
 #pragma unroll
@@ -155,7 +156,7 @@ __global__ __launch_bounds__(256) void w4_join_kernel(W4Params p) {
 template <typename T, int G, int MT, bool GATE>
 hipError_t launch(const W4Params& p, hipStream_t s) {
   const dim3 grid((p.tiles + kWaves - 1) / kWaves, p.splits, (p.m + 16 * MT - 1) / (16 * MT)), block(64 * kWaves);
-  if (p.vec) hipLaunchKernelGGL((w4_rows_kernel<T, G, MT, GATE, true>), grid, block, 0, s, p);
+  if (p.k >= 8) hipLaunchKernelGGL((w4_rows_kernel<T, G, MT, GATE, true>), grid, block, 0, s, p);
   else hipLaunchKernelGGL((w4_rows_kernel<T, G, MT, GATE, false>), grid, block, 0, s, p);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;

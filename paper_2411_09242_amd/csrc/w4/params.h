@@ -23,7 +23,6 @@ struct W4Params {
   void* out;           // of the product, or the matrix read
   int64_t xs, as, os;  // their rows' strides in elements
   int32_t m;           // rows of x
-  int32_t vec;         // x's rows start on 16-byte addresses and have a multiple of 8 channels
   // up to 16 rows
   int32_t wide;   // two tiles to a workgroup
   int32_t waves;  // wavefronts that share a tile's channels

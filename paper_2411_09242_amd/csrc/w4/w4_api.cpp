@@ -152,7 +152,6 @@ fluid_status fluid_w4_matmul(const fluid_w4* w, const void* packed, const void* 
     p.x = x;
     p.add = add;
     p.out = out;
-    p.vec = (uintptr_t)x % 16 == 0 && (p.xs * dtype_bytes(xd->dtype)) % 16 == 0 && p.k % 8 == 0;
     const uint64_t need = workspace_of(p, gate != nullptr);
     if (need) {
       if (workspace == nullptr || workspace_bytes < need)

@@ -27,14 +27,21 @@ template <>
 struct Rows<uint16_t> {
   static constexpr int N = 1;
   static constexpr float OFFSET = 16.0f;
+  typedef uint32_t unaligned __attribute__((ext_vector_type(4), aligned(2)));
   u32x4 raw;
-  __device__ __forceinline__ void load(const uint16_t* x) { raw = *(const u32x4*)x; }
+  __device__ __forceinline__ void load(const uint16_t* x) { raw = *(const unaligned*)x; }
   __device__ __forceinline__ void load(const uint16_t* x, int left) {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
       raw[i] = (2 * i < left ? x[2 * i] : 0u) | (2 * i + 1 < left ? (uint32_t)x[2 * i + 1] << 16 : 0u);
   }
-  __device__ __forceinline__ void clear() { raw = u32x4{}; }
+  // without the first n channels, zeros behind the others
+  __device__ __forceinline__ void drop(int n) {
+    if (n & 1) raw = u32x4{raw[0] >> 16 | raw[1] << 16, raw[1] >> 16 | raw[2] << 16, raw[2] >> 16 | raw[3] << 16, raw[3] >> 16};
+    if (n & 2) raw = u32x4{raw[1], raw[2], raw[3], 0};
+    if (n & 4) raw = u32x4{raw[2], raw[3], 0, 0};
+    if (n >= 8) raw = u32x4{};
+  }
   __device__ __forceinline__ void parts(u32x4 p[N]) const { p[0] = raw; }
   __device__ static __forceinline__ u32x4 levels(uint32_t w) {
     constexpr uint32_t mask = 0x00780078, sixteen = 0x41804180;
@@ -48,13 +55,27 @@ struct Rows<float> {
   // about zero, so that a group's sums are no larger than they need be: with 16 + n
   // the error of 4096 channels was 2.5 times that of an fp32 product
   static constexpr float OFFSET = -8.0f;
+  typedef float unaligned __attribute__((ext_vector_type(4), aligned(4)));
   f32x4 raw[2];
-  __device__ __forceinline__ void load(const float* x) { raw[0] = ((const f32x4*)x)[0], raw[1] = ((const f32x4*)x)[1]; }
+  __device__ __forceinline__ void load(const float* x) {
+    raw[0] = ((const unaligned*)x)[0], raw[1] = ((const unaligned*)x)[1];
+  }
   __device__ __forceinline__ void load(const float* x, int left) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) raw[e >> 2][e & 3] = e < left ? x[e] : 0.0f;
   }
-  __device__ __forceinline__ void clear() { raw[0] = raw[1] = f32x4{}; }
+  __device__ __forceinline__ void drop(int n) {
+    if (n & 1) {
+      raw[0] = f32x4{raw[0][1], raw[0][2], raw[0][3], raw[1][0]};
+      raw[1] = f32x4{raw[1][1], raw[1][2], raw[1][3], 0.0f};
+    }
+    if (n & 2) {
+      raw[0] = f32x4{raw[0][2], raw[0][3], raw[1][0], raw[1][1]};
+      raw[1] = f32x4{raw[1][2], raw[1][3], 0.0f, 0.0f};
+    }
+    if (n & 4) raw[0] = raw[1], raw[1] = f32x4{};
+    if (n >= 8) raw[0] = raw[1] = f32x4{};
+  }
   // the first two parts are cut off, so that what is left is exact
   __device__ __forceinline__ void parts(u32x4 p[N]) const {
 #pragma unroll
