@@ -8,7 +8,7 @@
 //
 // A thread has a few neighbouring pairs of one token, and their angles once for
 // some of its heads.  Bound by memory, every value read and written once: 8192
-// tokens of 40 heads of 128 in bf16, 168 MB, in 36 us (4.6 TB/s; a copy of 4 GiB has
+// tokens of 40 heads of 128 in bf16, 168 MB, in 35 us (4.8 TB/s; a copy of 4 GiB has
 // 4.7).  One token takes 3 us, the launch and two dependent loads.
 #include "dev_attn.h"
 #include "launch_attn.h"
@@ -39,31 +39,42 @@ __device__ __forceinline__ void sin_cos(uint64_t turn, float& s, float& c) {
   c = (quarter + 1) & 2 ? -v : v;
 }
 
-// N neighbouring channels; with N > 1 they fill 16 bytes.
+// N neighbouring channels, loaded and stored at once.
 template <typename T, int N>
 struct Run {
   float x[N];
+  typedef T bits __attribute__((ext_vector_type(N)));
   __device__ __forceinline__ void load(const T* p) {
     if constexpr (N == 1) {
       x[0] = Elem<T>::load(p, 0);
-    } else if constexpr (sizeof(T) == 4) {
-      const f32x4 v = *(const f32x4*)p;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] = v[i];
     } else {
-      Eight<uint16_t> v;
-      v.load(p, true);
-      v.floats(x);
+      const bits v = *(const bits*)p;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const T e = v[i];
+        x[i] = Elem<T>::load(&e, 0);
+      }
     }
   }
   __device__ __forceinline__ void store(T* p) const {
-    if constexpr (N == 1) Elem<T>::store(p, 0, x[0]);
-    else if constexpr (sizeof(T) == 4) *(f32x4*)p = f32x4{x[0], x[1], x[2], x[3]};
-    else store8(p, true, x);
+    if constexpr (N == 1) {
+      Elem<T>::store(p, 0, x[0]);
+    } else if constexpr (sizeof(T) == 4) {
+      bits v;
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] = x[i];
+      *(bits*)p = v;
+    } else {
+      typedef uint32_t words __attribute__((ext_vector_type(N / 2)));
+      words v;
+#pragma unroll
+      for (int i = 0; i < N / 2; ++i) v[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
+      *(words*)p = v;
+    }
   }
 };
 
-// N: channels at once, 16 bytes of them or one
+// N: channels at once
 template <typename T, int N, bool INTER>
 __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams p) {
   constexpr int P = INTER && N > 1 ? N / 2 : N;  // pairs of a thread
@@ -95,8 +106,8 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams p) {
     T* const y = (T*)ya.p + (b * ya.sb + t * ya.st + at * ya.sh);
     if (!turned) {
       const int ch = p.dim + (unit - p.pairs) * N;
-      if constexpr (N == 1) y[ch] = x[ch];
-      else *(uint4*)(y + ch) = *(const uint4*)(x + ch);
+      typedef T bits __attribute__((ext_vector_type(N)));
+      *(bits*)(y + ch) = *(const bits*)(x + ch);
     } else if constexpr (INTER) {
       constexpr int C = 2 * P;
       float v[C], w[C];
@@ -150,8 +161,13 @@ hipError_t launch(const RotaryParams& p, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_rotate(const RotaryParams& p, int dtype, hipStream_t s) {
-  if (dtype == DT_BF16) return p.vec ? launch<uint16_t, 8>(p, s) : launch<uint16_t, 1>(p, s);
-  return p.vec ? launch<float, 4>(p, s) : launch<float, 1>(p, s);
+  const bool bf16 = dtype == DT_BF16;
+  switch (p.vec) {
+    case 8: return launch<uint16_t, 8>(p, s);  // of two bytes
+    case 4: return bf16 ? launch<uint16_t, 4>(p, s) : launch<float, 4>(p, s);
+    case 2: return bf16 ? launch<uint16_t, 2>(p, s) : launch<float, 2>(p, s);
+    default: return bf16 ? launch<uint16_t, 1>(p, s) : launch<float, 1>(p, s);
+  }
 }
 
 }  // namespace fluid

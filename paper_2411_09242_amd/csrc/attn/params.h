@@ -71,7 +71,7 @@ struct RotaryParams {
   int32_t batch, tokens, head_dim, dim;
   int32_t interleaved, inverse, tail;  // tail: channels behind dim are copied
   float amplitude;
-  int32_t vec;           // 16 bytes at a time
+  int32_t vec;           // channels at a time, a power of two, 16 bytes of them at most
   int32_t units, pairs;  // of a head: in all, of turned ones
   int32_t head_threads;  // that share a token's heads
   uint32_t items;        // threads

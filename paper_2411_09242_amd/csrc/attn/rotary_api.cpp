@@ -43,6 +43,14 @@ uint64_t turns_of(const fluid_rotary& r, int i) {
   return part < 0x1p64L ? (uint64_t)part : 0;  // also where a turn that no number holds makes a NaN
 }
 
+// Channels that can be read and written at once: bytes of them that divide the
+// address and all strides, at most 16.  4096 tokens of 40 heads of 80, bf16, half of
+// each turned: four at once, 14 us; one by one 28.
+int at_once(const TokensArg& a, int el) {
+  const uint64_t all = (uint64_t)(uintptr_t)a.p | (uint64_t)(a.sb * el) | (uint64_t)(a.st * el) | (uint64_t)(a.sh * el) | 16;
+  return (int)(all & -all) / el;
+}
+
 // q or k and where it goes.
 void set_pair(RotaryParams& p, int i, const fluid_tokens* xd, const void* x, const fluid_tokens* yd, void* y,
               const char* in, const char* out) {
@@ -58,7 +66,8 @@ void set_pair(RotaryParams& p, int i, const fluid_tokens* xd, const void* x, con
   else
     p.tail = 1;
   p.heads[i] = xd->heads;
-  p.vec &= a.vec & b.vec;
+  const int el = dtype_bytes(xd->dtype);
+  p.vec = std::min({p.vec, at_once(a, el), at_once(b, el)});
 }
 
 }  // namespace
@@ -84,7 +93,7 @@ fluid_status fluid_rotate(const fluid_rotary* r, const uint64_t* turns, const in
   return call_guarded([&] {
     check_rotary(r);
     RotaryParams p{};
-    p.vec = 1;
+    p.vec = 16;
     require(turns != nullptr && (uintptr_t)turns % 8 == 0, "turns: NULL or misaligned");
     require(start == nullptr || positions == nullptr, "start and positions: only one of them");
     require(inverse == 0 || inverse == 1, "inverse must be 0 or 1");
@@ -110,15 +119,13 @@ fluid_status fluid_rotate(const fluid_rotary* r, const uint64_t* turns, const in
     p.inverse = inverse;
     p.amplitude = r->amplitude;
     if (p.head_dim == p.dim) p.tail = 0;
-    const int wide = 16 / dtype_bytes(qd->dtype);  // channels of 16 bytes
-    if ((r->interleaved ? r->dim : r->dim / 2) % wide || (p.tail && p.head_dim % wide)) p.vec = 0;
-    const int at_once = p.vec ? wide : 1;
-    p.pairs = r->interleaved ? r->dim / (p.vec ? wide : 2) : r->dim / 2 / at_once;
-    p.units = p.pairs + (p.tail ? (p.head_dim - p.dim) / at_once : 0);
+    while ((r->interleaved ? r->dim : r->dim / 2) % p.vec || (p.tail && p.head_dim % p.vec)) p.vec /= 2;
+    p.pairs = r->interleaved ? r->dim / std::max(p.vec, 2) : r->dim / 2 / p.vec;
+    p.units = p.pairs + (p.tail ? (p.head_dim - p.dim) / p.vec : 0);
     const int64_t heads = int64_t(p.heads[0]) + p.heads[1], rows = product({p.batch, p.tokens, p.units});
     // A thread's angles serve up to four heads where that still fills the GPU: 8192
-    // tokens of 40 heads take 36.2 us, with eight heads to a thread 37.7 and two 39.3
-    // (2048 tokens 10.5, 11.6, 9.9); 1024 tokens of 40 heads 7.5 us with a thread to a
+    // tokens of 40 heads take 35 us, with eight heads to a thread 37 and two 38 (2048
+    // tokens 10.5, 11.6, 9.9); 1024 tokens of 40 heads 7.5 us with a thread to a
     // head, 8.2 to 11.5 with four.
     const int64_t few = (heads + 3) / 4;
     p.head_threads = (int32_t)(product({rows, few}) >= 131072 ? few : heads);

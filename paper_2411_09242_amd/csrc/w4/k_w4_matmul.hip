@@ -15,9 +15,8 @@ namespace fluid {
 
 namespace {
 
-// NT: tiles of 16 rows of the matrix.  VEC: x has eight channels or more, which are
-// loaded at once; the last ones end with the row.
-template <typename T, int G, int NT, bool GATE, bool VEC>
+// NT: tiles of 16 rows of the matrix.
+template <typename T, int G, int NT, bool GATE, Load HOW>
 __global__ __launch_bounds__(GATE || NT == 2 || sizeof(T) == 4 ? 512 : 1024) void w4_few_kernel(W4Params p) {
   constexpr int MATS = GATE ? 2 : 1, GROUPS = 128 / G, STEPS = G / 32, P = Rows<T>::N;
   extern __shared__ float sums[];  // [wavefront][matrix][tile][256]
@@ -31,7 +30,7 @@ __global__ __launch_bounds__(GATE || NT == 2 || sizeof(T) == 4 ? 512 : 1024) voi
   struct Block {
     u32x4 w[MATS][NT];
     f16x2 sb[MATS][NT][GROUPS];
-    Rows<T> x[4];
+    Piece<T, HOW> x[4];
   };
   auto fetch = [&](int c, Block& to) {
 #pragma unroll
@@ -46,19 +45,14 @@ __global__ __launch_bounds__(GATE || NT == 2 || sizeof(T) == 4 ? 512 : 1024) voi
       }
     const T* const x = (const T*)p.x + row * p.xs;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int ch = 128 * c + 32 * j + 8 * g;
-      if constexpr (VEC) to.x[j].load(x + min(ch, p.k - 8));
-      else to.x[j].load(x + ch, p.k - ch);
-    }
+    for (int j = 0; j < 4; ++j) to.x[j].fetch(x, 128 * c + 32 * j + 8 * g, p.k);
   };
 
   f32x4 y[MATS][NT] = {};
   auto multiply = [&](int c, Block& in) {
-    if (VEC && 128 * c + 128 > p.k) {
+    const bool end = 128 * c + 128 > p.k;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) in.x[j].drop(max(128 * c + 32 * j + 8 * g - (p.k - 8), 0));
-    }
+    for (int j = 0; j < 4; ++j) in.x[j].settle(128 * c + 32 * j + 8 * g, p.k, end);
 #pragma unroll
     for (int i = 0; i < GROUPS; ++i) {
       f32x4 part[MATS][NT] = {}, all = {};
@@ -122,8 +116,10 @@ template <typename T, int G, int NT, bool GATE>
 hipError_t launch(const W4Params& p, hipStream_t s) {
   const dim3 grid((p.tiles + NT - 1) / NT), block(64 * p.waves);
   const int lds = p.waves * (GATE ? 2 : 1) * NT * 1024;
-  if (p.k >= 8) hipLaunchKernelGGL((w4_few_kernel<T, G, NT, GATE, true>), grid, block, lds, s, p);
-  else hipLaunchKernelGGL((w4_few_kernel<T, G, NT, GATE, false>), grid, block, lds, s, p);
+  if (p.k < 8) hipLaunchKernelGGL((w4_few_kernel<T, G, NT, GATE, kOneByOne>), grid, block, lds, s, p);
+  else if (!by_words<T>(p)) hipLaunchKernelGGL((w4_few_kernel<T, G, NT, GATE, kAtOnce>), grid, block, lds, s, p);
+  else if constexpr (sizeof(T) == 2)
+    hipLaunchKernelGGL((w4_few_kernel<T, G, NT, GATE, kByWords>), grid, block, lds, s, p);
   return hipGetLastError();
 }
 template <typename T, int G, bool GATE>

@@ -19,9 +19,8 @@ namespace {
 
 constexpr int kWaves = 8;
 
-// MT: tiles of 16 rows of x.  VEC: x has eight channels or more, which are loaded at
-// once; the last ones end with the row.
-template <typename T, int G, int MT, bool GATE, bool VEC>
+// MT: tiles of 16 rows of x.
+template <typename T, int G, int MT, bool GATE, Load HOW>
 __global__ __launch_bounds__(64 * kWaves) void w4_rows_kernel(W4Params p) {
   constexpr int MATS = GATE ? 2 : 1, GROUPS = 128 / G, STEPS = G / 32, P = Rows<T>::N;
   constexpr int PIECES = MT * 4 / kWaves;  // of x, of a thread
@@ -45,23 +44,22 @@ __global__ __launch_bounds__(64 * kWaves) void w4_rows_kernel(W4Params p) {
       load_pairs<GROUPS>(of.pairs + at * (64 * GROUPS) + r * (4 * GROUPS), to.sb[a]);
     }
   };
+  typedef Piece<T, HOW> X;
   // a thread's pieces: of step and tile wave + kWaves i, lane's place
   auto channel = [&](int c, int i) { return 128 * c + 32 * ((wave + kWaves * i) / MT) + 8 * g; };
-  auto fetch_x = [&](int c, Rows<T> to[PIECES]) {
+  auto fetch_x = [&](int c, X to[PIECES]) {
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
       // rows behind the last are not stored, channels behind the last dropped below
-      const int row = min(m0 + 16 * ((wave + kWaves * i) % MT) + r, p.m - 1), ch = channel(c, i);
-      const T* const x = (const T*)p.x + row * p.xs;
-      if constexpr (VEC) to[i].load(x + min(ch, p.k - 8));
-      else to[i].load(x + ch, p.k - ch);
+      const int row = min(m0 + 16 * ((wave + kWaves * i) % MT) + r, p.m - 1);
+      to[i].fetch((const T*)p.x + row * p.xs, channel(c, i), p.k);
     }
   };
-  auto put = [&](int c, Rows<T> from[PIECES], u32x4* to) {
+  auto put = [&](int c, X from[PIECES], u32x4* to) {
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
       const int u = wave + kWaves * i;
-      if (VEC && 128 * c + 128 > p.k) from[i].drop(max(channel(c, i) - (p.k - 8), 0));
+      from[i].settle(channel(c, i), p.k, 128 * c + 128 > p.k);
       u32x4 part[P];
       from[i].parts(part);
 #pragma unroll
@@ -101,7 +99,7 @@ __global__ __launch_bounds__(64 * kWaves) void w4_rows_kernel(W4Params p) {
   // The last block is loaded again rather than nothing: behind a branch that may
   // have loads or not, the compiler waits for all of them.
   Words words[4];
-  Rows<T> xr[2][PIECES];
+  X xr[2][PIECES];
   const int last = past - 1;
   fetch_x(first, xr[0]);
 #pragma unroll
@@ -156,8 +154,10 @@ __global__ __launch_bounds__(256) void w4_join_kernel(W4Params p) {
 template <typename T, int G, int MT, bool GATE>
 hipError_t launch(const W4Params& p, hipStream_t s) {
   const dim3 grid((p.tiles + kWaves - 1) / kWaves, p.splits, (p.m + 16 * MT - 1) / (16 * MT)), block(64 * kWaves);
-  if (p.k >= 8) hipLaunchKernelGGL((w4_rows_kernel<T, G, MT, GATE, true>), grid, block, 0, s, p);
-  else hipLaunchKernelGGL((w4_rows_kernel<T, G, MT, GATE, false>), grid, block, 0, s, p);
+  if (p.k < 8) hipLaunchKernelGGL((w4_rows_kernel<T, G, MT, GATE, kOneByOne>), grid, block, 0, s, p);
+  else if (!by_words<T>(p)) hipLaunchKernelGGL((w4_rows_kernel<T, G, MT, GATE, kAtOnce>), grid, block, 0, s, p);
+  else if constexpr (sizeof(T) == 2)
+    hipLaunchKernelGGL((w4_rows_kernel<T, G, MT, GATE, kByWords>), grid, block, 0, s, p);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
   hipLaunchKernelGGL((w4_join_kernel<T, GATE>), dim3((p.n + 255) / 256, p.m), dim3(256), 0, s, p);

@@ -100,6 +100,44 @@ struct Rows<float> {
   }
 };
 
+// How eight channels of a row of x are loaded: one by one (rows of fewer than eight);
+// at once, the row's last ones from where they end with it; or, where rows start at
+// odd halves of a word, as the words that hold them (16 bytes at such an address took
+// 8 rows of 4095 channels from 5 to 14 us).
+enum Load { kOneByOne, kAtOnce, kByWords };
+
+template <typename T, Load HOW>
+struct Piece : Rows<T> {
+  __device__ __forceinline__ void fetch(const T* row, int ch, int k) {
+    if constexpr (HOW == kOneByOne) this->load(row + ch, k - ch);
+    else this->load(row + min(ch, k - 8));
+  }
+  // before use; last: the block ends behind the row
+  __device__ __forceinline__ void settle(int ch, int k, bool last) {
+    if (HOW != kOneByOne && last) this->drop(max(ch - (k - 8), 0));
+  }
+};
+template <>
+struct Piece<uint16_t, kByWords> : Rows<uint16_t> {
+  uint32_t end, shift;
+  __device__ __forceinline__ void fetch(const uint16_t* row, int ch, int k) {
+    typedef uint32_t words __attribute__((ext_vector_type(4), aligned(4)));
+    const uintptr_t at = (uintptr_t)(row + min(ch, k - 8));
+    raw = *(const words*)(at & ~uintptr_t(3));
+    end = *(const uint32_t*)((at + 14) & ~uintptr_t(3));  // the word of the last channel
+    shift = (at & 2) * 8;
+  }
+  __device__ __forceinline__ void settle(int ch, int k, bool last) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) raw[i] = __builtin_amdgcn_alignbit(i < 3 ? raw[i + 1] : end, raw[i], shift);
+    if (last) drop(max(ch - (k - 8), 0));
+  }
+};
+template <typename T>
+inline bool by_words(const W4Params& p) {
+  return sizeof(T) == 2 && ((uintptr_t)p.x % 4 || p.xs % 2);
+}
+
 // A group's sums of x times levels, and of x, into y.
 template <typename T>
 __device__ __forceinline__ void add_group(f16x2 sb, f32x4 part, f32x4 all, f32x4& y) {

@@ -170,6 +170,22 @@ def test_strides_dimensions_and_outputs(dtype):
     assert torch.equal(y, W.w4_matmul(one, w).expand(4, N))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M", [1, 3, 16, 21, 40])
+def test_rows_of_every_length_and_alignment(dtype, M):
+    """Pieces of eight channels that end with the row, words that start between two
+    rows; what lies beside the rows is no number."""
+    N, group = 19, 32
+    for K in (1, 5, 7, 8, 9, 15, 16, 100, 127, 131, 136, 255):
+        parts = matrix(K, N, K, group)
+        w = w4_of(*parts, group)
+        for off, pad in ((0, 0), (1, 2), (2, 5), (3, 4)):
+            buf = torch.full((M * (K + pad) + 8,), float("nan"), dtype=DT[dtype], device="cuda")
+            x = buf[off:off + M * (K + pad)].view(M, K + pad)[:, :K]
+            x.copy_(rand(3 + K, M, K, dtype=dtype))
+            check(W.w4_matmul(x, w), x, parts, group, dtype)
+
+
 def test_rows_do_not_touch_each_other():
     """A row that is no number makes none of the others so, and a row's result
     does not depend on what is beside it."""
