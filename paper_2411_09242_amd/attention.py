@@ -431,7 +431,8 @@ def linear_attention(q, k, v, decay, state=None, count=None, scale=None, out=Non
     [kv_heads] or one a token [batch, T, kv_heads].  state: fp32 [batch, kv_heads,
     head_dim, head_dim] to start from (None: zeros); state_out: where to leave the
     last one, which may be ``state`` (allocated by default).  count[b] (None: T)
-    tokens of sequence b are there; out's rows behind them are left as they are.
+    tokens of sequence b are there; out's rows behind them are left as they are, and
+    out must not overlap an input.
     scale: 1 / sqrt(head_dim) by default.  A prompt and the single tokens behind
     it are calls that hand the state on.  Returns (out, state_out)."""
     if out is None:

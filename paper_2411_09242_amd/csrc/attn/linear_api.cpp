@@ -89,6 +89,12 @@ fluid_status fluid_linear_attention(float scale, const fluid_tokens* qd, const v
     for (int i = 0; i < 3; ++i)
       require(decay_stride[i] >= 0 && decay_stride[i] <= (int64_t(1) << 40), "decay: strides must lie in 0 .. 2^40");
     require((uintptr_t)state % 16 == 0 && (uintptr_t)state_out % 16 == 0, "state: must be 16-byte aligned");
+    // workgroups read these while others write
+    require(out != q && out != k && out != v, "out: must not be q, k or v");
+    const uintptr_t from = (uintptr_t)state, to = (uintptr_t)state_out,
+                    bytes = (uintptr_t)product({p.batch, p.kv_heads, qd->head_dim, qd->head_dim, 4});
+    require(!state || !state_out || from == to || (from < to ? to - from : from - to) >= bytes,
+            "state_out: must be state or apart from it");
     p.q = qa;
     p.k = ka;
     p.v = va;

@@ -133,7 +133,7 @@ def test_oracle_rotation_pins():
 
 # -------------------------------------------------------- linear attention
 def linear(scale=0.5, qd=None, q=ADDR, kd=None, k=ADDR, vd=None, v=ADDR, decay=ADDR, stride=(0, 0, 1), state=ADDR, count=None,
-           od=None, out=ADDR, state_out=ADDR, ws=ADDR, ws_bytes=1 << 40):
+           od=None, out=ADDR + (1 << 24), state_out=ADDR, ws=ADDR, ws_bytes=1 << 40):
     qd = qd or tokens()
     kd = kd or tokens(heads=2)
     stride = None if stride is None else (C.c_int64 * 3)(*stride)
@@ -143,7 +143,8 @@ def linear(scale=0.5, qd=None, q=ADDR, kd=None, k=ADDR, vd=None, v=ADDR, decay=A
 
 
 def test_right_linear_calls_reach_the_gpu_part():
-    for kw in (dict(), dict(state=None, state_out=None), dict(count=ADDR), dict(stride=(10, 2, 1)), dict(scale=-1.0),
+    for kw in (dict(), dict(state=None, state_out=None), dict(count=ADDR),
+               dict(state_out=ADDR + 2 * 2 * 64 * 64 * 4), dict(state=ADDR + 2 * 2 * 64 * 64 * 4), dict(stride=(10, 2, 1)), dict(scale=-1.0),
                dict(qd=tokens(tokens=3000), kd=tokens(tokens=3000, heads=1)),
                dict(qd=tokens(dtype=F.F32, head_dim=128), kd=tokens(dtype=F.F32, head_dim=128, heads=4))):
         st, msg = linear(**kw)
@@ -157,6 +158,8 @@ def test_right_linear_calls_reach_the_gpu_part():
     (dict(state_out=ADDR + 8), "aligned"), (dict(kd=tokens(heads=3)), "multiple"), (dict(kd=tokens(heads=2, tokens=6)), "one dtype"),
     (dict(kd=tokens(heads=2, dtype=F.F32)), "one dtype"), (dict(vd=tokens(heads=1)), "one dtype and shape"),
     (dict(od=tokens(tokens=6)), "out"), (dict(od=tokens(stride=(1280, 0, 64))), "head_dim"),
+    *((dict(out=ADDR + (2 << 24), **{name: ADDR + (2 << 24)}), "must not be q, k or v") for name in "qkv"),
+    (dict(state_out=ADDR + 2 * 2 * 64 * 64 * 4 - 16), "apart"), (dict(state=ADDR + 16), "apart"),
     (dict(qd=tokens(head_dim=48), kd=tokens(head_dim=48, heads=2)), "head_dim"), (dict(qd=tokens(tokens=0)), "at least 1"),
     (dict(qd=tokens(batch=1 << 20, heads=64, stride=(0, 0, 0)), kd=tokens(batch=1 << 20, heads=64, stride=(0, 0, 0)),
           od=tokens(batch=1 << 20, heads=64, stride=(1 << 20, 1 << 14, 64))), "too large"),

@@ -214,6 +214,26 @@ def test_what_is_no_number_reaches_only_what_follows(dtype):
                     assert torch.equal(out[0, 71:], clean[0][0, 71:]) and torch.equal(last, clean[1])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T, heads, at", [(2, 1, 1), (3, 2, 1), (150, 1, 70), (900, 2, 0), (900, 2, 333)])
+def test_a_decay_that_is_no_number_reaches_what_follows(dtype, T, heads, at):
+    """All channels of its head's rows from it on and its state; nothing else."""
+    B, Hk, D = 2, 2, 64
+    q = rand(1, B, T, heads * Hk, D, dtype=dtype)
+    k, v = rand(2, B, T, Hk, D, dtype=dtype), rand(3, B, T, Hk, D, dtype=dtype)
+    g, state = decays(4, B, T, Hk, True).clamp(min=-5.0), rand(5, B, Hk, D, D)
+    run = lambda: A.linear_attention(q, k, v, g, state=state, scale=0.2)  # noqa: E731
+    clean = run()
+    for value in (float("nan"), float("inf")):
+        g[0, at, 1] = value
+        out, last = run()
+        mine = slice(heads, 2 * heads)
+        assert not out[0, at:, mine].isfinite().any() and not last[0, 1].isfinite().any()
+        assert torch.equal(out[0, :at], clean[0][0, :at]) and torch.equal(out[0, :, :heads], clean[0][0, :, :heads])
+        assert torch.equal(out[1], clean[0][1]) and torch.equal(last[1], clean[1][1])
+        assert torch.equal(last[0, 0], clean[1][0, 0])
+
+
 def test_a_decay_of_nothing_forgets_everything():
     B, T, H, D = 1, 90, 1, 32
     q, k, v = (rand(i, B, T, H, D) for i in (1, 2, 3))
