@@ -62,14 +62,14 @@ fluid_status fluid_w4_read(const fluid_w4* w, const void* packed, const fluid_ma
  * (with ad): NULL for none.  out may be add itself with the same stride, and must
  * not overlap x.  Made for few rows: every 64 of them read the matrix again.
  * workspace: 256-byte aligned device memory of at least the bytes that
- * fluid_w4_matmul_workspace returns for M rows (0: NULL will do), for this call
+ * fluid_w4_matmul_workspace returns for x (0: NULL will do), for this call
  * alone while it runs.
  * Arithmetic: x times 16 + n on the bf16 matrix cores (fp32: n - 8, and x in three
  * bf16 parts, exact to 2^-23), fp32 sums over a group, which s and b then enter in
  * fp32; one rounding at the end.  A row of x that is not finite, or whose sums
  * times 31 pass fp32, gives NaN or infinities in that row alone.  Errors:
  * FLUID_E_INVALID; FLUID_E_ARENA_TOO_SMALL (workspace). */
-fluid_status fluid_w4_matmul_workspace(const fluid_w4* w, int32_t rows, int32_t gated, uint64_t* bytes);
+fluid_status fluid_w4_matmul_workspace(const fluid_w4* w, const fluid_matrix* xd, int32_t gated, uint64_t* bytes);
 fluid_status fluid_w4_matmul(const fluid_w4* w, const void* packed, const void* gate, const fluid_matrix* xd,
                              const void* x, const fluid_matrix* ad, const void* add, const fluid_matrix* od, void* out,
                              void* workspace, uint64_t workspace_bytes, void* hip_stream);

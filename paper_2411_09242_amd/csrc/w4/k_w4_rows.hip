@@ -6,10 +6,10 @@
 // Where that are too few workgroups, runs of channels go to workgroups of their own,
 // whose sums a second launch adds in order.
 //
-// 32 rows times 4096 x 11008: 16.7 us, 12.5 and 4 in the two launches; with x from L2
-// for every 32 rows of the matrix, one launch, 25.  Vector instructions (levels, and
-// sums times s and b) take 4.4 us, the words' first loads and the sums' way to memory
-// most of the rest.  64 rows 23 us.
+// 64 rows times 4096 x 11008: 23 us, 4 of them the second launch; 32 fp32 rows 25.6 us
+// (x in pieces of 64 bytes of a row, not 256: 26.2; 4096 x 4096 15.5 and 16.4).  Vector
+// instructions (levels, and sums times s and b), the words' first loads and the sums'
+// way to memory are most of it.
 #include "launch_w4.h"
 #include "w4_tile.h"
 
@@ -25,7 +25,9 @@ __global__ __launch_bounds__(64 * kWaves) void w4_rows_kernel(W4Params p) {
   constexpr int MATS = GATE ? 2 : 1, GROUPS = 128 / G, STEPS = G / 32, P = Rows<T>::N;
   constexpr int PIECES = MT * 4 / kWaves;  // of x, of a thread
   static_assert(PIECES * kWaves == MT * 4, "whole pieces");
-  __shared__ u32x4 sx[2][4 * MT * P * 64];  // [step][tile][part][lane]
+  // [step][tile][part][16 g + (r ^ piece)], a piece being 4 step + g: what is written, 16
+  // pieces of a row, and what is read, one of 16 rows, both meet all banks
+  __shared__ u32x4 sx[2][4 * MT * P * 64];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
   const int tile = blockIdx.x * kWaves + wave, m0 = blockIdx.z * (16 * MT);
   const int first = blockIdx.y * p.run, past = min(first + p.run, p.blocks);
@@ -45,26 +47,27 @@ __global__ __launch_bounds__(64 * kWaves) void w4_rows_kernel(W4Params p) {
     }
   };
   typedef Piece<T, HOW> X;
-  // a thread's pieces: of step and tile wave + kWaves i, lane's place
-  auto channel = [&](int c, int i) { return 128 * c + 32 * ((wave + kWaves * i) / MT) + 8 * g; };
+  // a thread's pieces: eight channels each, a wavefront's 256 bytes of each of the four
+  // rows from 4 (wave + kWaves i) on
+  const int ch = 8 * r;
   auto fetch_x = [&](int c, X to[PIECES]) {
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
       // rows behind the last are not stored, channels behind the last dropped below
-      const int row = min(m0 + 16 * ((wave + kWaves * i) % MT) + r, p.m - 1);
-      to[i].fetch((const T*)p.x + row * p.xs, channel(c, i), p.k);
+      const int row = min(m0 + 4 * (wave + kWaves * i) + g, p.m - 1);
+      to[i].fetch((const T*)p.x + row * p.xs, 128 * c + ch, p.k);
     }
   };
   auto put = [&](int c, X from[PIECES], u32x4* to) {
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
       const int u = wave + kWaves * i;
-      from[i].settle(channel(c, i), p.k, 128 * c + 128 > p.k);
+      from[i].settle(128 * c + ch, p.k, 128 * c + 128 > p.k);
       u32x4 part[P];
       from[i].parts(part);
 #pragma unroll
       for (int k = 0; k < P; ++k)
-        to[(u * P + k) * 64 + lane] = part[k];
+        to[((r / 4 * MT + u / 4) * P + k) * 64 + 16 * (r % 4) + ((4 * (u % 4) + g) ^ r)] = part[k];
     }
   };
 
@@ -82,7 +85,7 @@ __global__ __launch_bounds__(64 * kWaves) void w4_rows_kernel(W4Params p) {
         for (int t = 0; t < MT; ++t)
 #pragma unroll
           for (int k = 0; k < P; ++k) {
-            const u32x4 of = x[((j * MT + t) * P + k) * 64 + lane];
+            const u32x4 of = x[((j * MT + t) * P + k) * 64 + 16 * g + (r ^ (4 * j + g))];
             all[t] = mfma(of, ones, all[t]);
 #pragma unroll
             for (int a = 0; a < MATS; ++a) part[a][t] = mfma(of, l[a], part[a][t]);
@@ -166,7 +169,8 @@ hipError_t launch(const W4Params& p, hipStream_t s) {
 template <typename T, int G>
 hipError_t launch_rows(const W4Params& p, hipStream_t s) {
   const bool gate = p.gate.words != nullptr;
-  if (p.m <= 32) return gate ? launch<T, G, 2, true>(p, s) : launch<T, G, 2, false>(p, s);
+  if constexpr (sizeof(T) == 4)
+    if (p.m <= 32) return gate ? launch<T, G, 2, true>(p, s) : launch<T, G, 2, false>(p, s);
   return gate ? launch<T, G, 4, true>(p, s) : launch<T, G, 4, false>(p, s);
 }
 template <typename T>

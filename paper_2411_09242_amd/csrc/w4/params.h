@@ -23,11 +23,11 @@ struct W4Params {
   void* out;           // of the product, or the matrix read
   int64_t xs, as, os;  // their rows' strides in elements
   int32_t m;           // rows of x
-  // up to 16 rows
+  // few rows
   int32_t wide;   // two tiles to a workgroup
   int32_t waves;  // wavefronts that share a tile's channels
   // more
-  int32_t splits;  // runs of blocks that workgroups of their own take; 0: up to 16 rows
+  int32_t splits;  // runs of blocks that workgroups of their own take; 0: few rows
   int32_t run;     // blocks of a run
   float* ws;       // splits > 1: [run][matrix][row][output] sums
 };

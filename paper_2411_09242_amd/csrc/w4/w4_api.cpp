@@ -36,16 +36,20 @@ W4Arg held(const W4Params& p, const void* packed, const char* name) {
 }
 
 // Stride of a matrix's rows, in elements.
-int64_t check_matrix(const fluid_matrix* d, const void* data, int32_t cols, const char* name) {
+int64_t check_sizes(const fluid_matrix* d, int32_t cols, const char* name) {
   require(d != nullptr, name, ": NULL description");
-  require(data != nullptr, name, ": NULL data");
   require(d->dtype == FLUID_F32 || d->dtype == FLUID_BF16, name, ": dtype must be f32 or bf16");
-  require((uintptr_t)data % dtype_bytes(d->dtype) == 0, name, ": misaligned for its type");
   require(d->rows >= 1 && d->cols >= 1, name, ": rows and cols must be at least 1");
   require(d->cols == cols, name, ": cols do not fit the matrix");
   if (d->rows == 1) return 0;
   require(d->stride >= 0 && d->stride <= (int64_t(1) << 40), name, ": stride must lie in 0 .. 2^40");
   return d->stride;
+}
+int64_t check_matrix(const fluid_matrix* d, const void* data, int32_t cols, const char* name) {
+  const int64_t stride = check_sizes(d, cols, name);
+  require(data != nullptr, name, ": NULL data");
+  require((uintptr_t)data % dtype_bytes(d->dtype) == 0, name, ": misaligned for its type");
+  return stride;
 }
 void check_apart(const fluid_matrix* d, const char* name) {
   require(d->rows == 1 || d->stride >= d->cols, name, ": an output's stride must be at least its cols");
@@ -56,20 +60,22 @@ void plan_product(W4Params& p, int32_t rows, bool gate, int dtype) {
   p.m = rows;
   require(rows <= 64 * 65535, "x: too many rows for one launch");
   require(int64_t(p.tiles) * 1024 < int64_t(1) << 32, "w: too large for one launch");
-  if (rows <= 16) {
-    // Two tiles to a workgroup share x where there are enough: one row times 11008 x
-    // 4096 8.3 us, with one tile 9.4; 8192 x 4096 6.7 and 7.2, eight rows 7.2 and 10.2;
-    // 4096 x 11008, 256 tiles, 12.7 and 8.2 us.  Then, and with a gate, four wavefronts
-    // hold the registers for it (32000 x 1024 6.2 us, with eight 7.2); else sixteen,
-    // which take fewer blocks each (4096 x 11008 8.2 us, with eight 9.8).  fp32 x has no
-    // room for sixteen.
-    p.wide = p.tiles >= 512 && !gate;
+  // 4096 x 11008, 17 and 32 bf16 rows: 13.0 and 14.4 us in one launch, 16.6 in two; fp32,
+  // 32 rows: 37 and 25.6.
+  if (rows <= (dtype == FLUID_BF16 ? 32 : 16)) {
+    // Two tiles to a workgroup share x where there are enough: 8192 x 4096, eight rows 7.5
+    // us, with one tile 8.4; one row times 32000 x 4096 14.4 and 16.5, but 11008 x 4096
+    // 8.4 and 7.9; 4096 x 11008, 256 tiles, 11.8 and 7.1.  Then, and with a gate, four
+    // wavefronts hold the registers for it (32000 x 1024 6.7 us, with eight 7.3; 32 rows 12.2
+    // and 15.7); else sixteen, which take fewer blocks each (4096 x 11008, eight rows 8.4
+    // us, with eight 8.9).  fp32 x and 32 rows have no room for sixteen.
+    p.wide = p.tiles >= (rows > 4 ? 512 : 1024) && !gate;
     const bool many = gate || p.wide;
-    p.waves = p.blocks < 8 || (many && dtype == FLUID_BF16) ? 4 : p.blocks < 16 || dtype != FLUID_BF16 ? 8 : 16;
+    p.waves = p.blocks < 8 || (many && dtype == FLUID_BF16) ? 4 : p.blocks < 16 || rows > 16 || dtype != FLUID_BF16 ? 8 : 16;
     return;
   }
-  // As many runs as make a workgroup to a compute unit, of four blocks or more: 32
-  // rows times 4096 x 11008 take 16.7 us in 256 workgroups, 19.6 in 512, 22.7 in 128.
+  // As many runs as make a workgroup to a compute unit, of four blocks or more: 64
+  // rows times 4096 x 11008 take 23 us in 256 workgroups, 28 in 512, 30 in 128.
   const int64_t groups = (int64_t(p.tiles) + 7) / 8 * ((rows + 63) / 64);
   const int64_t runs = std::max<int64_t>(1, std::min<int64_t>(256 / groups, p.blocks / 4));
   p.run = (int32_t)((p.blocks + runs - 1) / runs);
@@ -120,13 +126,13 @@ fluid_status fluid_w4_read(const fluid_w4* w, const void* packed, const fluid_ma
   });
 }
 
-fluid_status fluid_w4_matmul_workspace(const fluid_w4* w, int32_t rows, int32_t gated, uint64_t* bytes) {
+fluid_status fluid_w4_matmul_workspace(const fluid_w4* w, const fluid_matrix* xd, int32_t gated, uint64_t* bytes) {
   return call_guarded([&] {
     W4Params p = check_shape(w);
-    require(rows >= 1, "rows must be at least 1");
+    check_sizes(xd, w->cols, "x");
     require(gated == 0 || gated == 1, "gated must be 0 or 1");
     require(bytes != nullptr, "bytes: NULL");
-    plan_product(p, rows, gated, FLUID_BF16);
+    plan_product(p, xd->rows, gated, xd->dtype);
     *bytes = workspace_of(p, gated);
   });
 }

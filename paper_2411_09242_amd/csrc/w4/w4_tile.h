@@ -42,6 +42,10 @@ struct Rows<uint16_t> {
     if (n & 4) raw = u32x4{raw[2], raw[3], 0, 0};
     if (n >= 8) raw = u32x4{};
   }
+  // in LDS
+  static constexpr int PLANES = 1;
+  __device__ __forceinline__ void put(u32x4* at, int plane) const { at[0] = raw; }
+  __device__ __forceinline__ void get(const u32x4* at, int plane) { raw = at[0]; }
   __device__ __forceinline__ void parts(u32x4 p[N]) const { p[0] = raw; }
   __device__ static __forceinline__ u32x4 levels(uint32_t w) {
     constexpr uint32_t mask = 0x00780078, sixteen = 0x41804180;
@@ -75,6 +79,15 @@ struct Rows<float> {
     }
     if (n & 4) raw[0] = raw[1], raw[1] = f32x4{};
     if (n >= 8) raw[0] = raw[1] = f32x4{};
+  }
+  static constexpr int PLANES = 2;
+  __device__ __forceinline__ void put(u32x4* at, int plane) const {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) at[i * plane] = __builtin_bit_cast(u32x4, raw[i]);
+  }
+  __device__ __forceinline__ void get(const u32x4* at, int plane) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) raw[i] = __builtin_bit_cast(f32x4, at[i * plane]);
   }
   // the first two parts are cut off, so that what is left is exact
   __device__ __forceinline__ void parts(u32x4 p[N]) const {

@@ -33,7 +33,7 @@ _PROTOS = {
     "fluid_w4_bytes": [_VP] * 2,
     "fluid_w4_pack": [_VP] * 5,
     "fluid_w4_read": [_VP] * 5,
-    "fluid_w4_matmul_workspace": [_VP, _I32, _I32, _VP],
+    "fluid_w4_matmul_workspace": [_VP, _VP, _I32, _VP],
     "fluid_w4_matmul": [_VP] * 10 + [_U64, _VP],
 }
 SYMBOLS = tuple(_PROTOS)
@@ -179,13 +179,13 @@ def _matmul_call(x, w, gate, add, out):
             _refuse(f"add: {shape} is needed, got {tuple(add.shape)}")
     if tuple(out.shape) != shape:
         _refuse(f"out: {shape} is needed, got {tuple(out.shape)}")
-    need = _need(w, xd.rows, gate is not None)
+    need = _need(w, xd, gate is not None)
     return (_lib(), dev, _addr(xd), None if ad is None else _addr(ad), _addr(od), need, (xd, ad, od))
 
 
-def _need(w, rows, gated):
+def _need(w, xd, gated):
     n = _U64()
-    fluid._check(_lib().fluid_w4_matmul_workspace(_addr(w.desc), rows, 1 if gated else 0, C.byref(n)))
+    fluid._check(_lib().fluid_w4_matmul_workspace(_addr(w.desc), _addr(xd), 1 if gated else 0, C.byref(n)))
     return n.value
 
 
@@ -193,7 +193,7 @@ def w4_matmul_workspace(x, w, gated=False):
     """Bytes of workspace that ``w4_matmul`` needs for these arguments."""
     dev = _device_of(x, "x")
     _check_w4(w, "w", dev)
-    return _need(w, _matrix(x, "x", dev).rows, gated)
+    return _need(w, _matrix(x, "x", dev), gated)
 
 
 def w4_matmul(x, w, gate=None, add=None, out=None, workspace=None, stream=None):

@@ -243,22 +243,26 @@ def test_product_refusals(bad, word):
 
 def test_product_workspace_is_checked():
     lib, n = W._lib(), C.c_uint64()
+    x = lambda rows, dtype=F.BF16: ref(matrix(rows=rows, cols=8192, dtype=dtype))  # noqa: E731
     w = shape(rows=512, cols=8192)
     kw = dict(w=w, xd=matrix(rows=40, cols=8192), od=matrix(rows=40, cols=512))
-    assert lib.fluid_w4_matmul_workspace(ref(w), 40, 0, C.byref(n)) == 0 and n.value > 0
+    assert lib.fluid_w4_matmul_workspace(ref(w), x(40), 0, C.byref(n)) == 0 and n.value > 0
     assert matmul(**kw, ws_bytes=n.value)[0] == UNSUPPORTED
     for bad in (dict(ws_bytes=n.value - 1), dict(ws=None)):
         st, msg = matmul(**kw, **bad)
         assert st == TOO_SMALL and "workspace" in msg
     st, msg = matmul(**kw, ws=ADDR + 16)
     assert st == INVALID and "aligned" in msg
-    assert lib.fluid_w4_matmul_workspace(ref(w), 40, 1, C.byref(n)) == 0 and matmul(**kw, gate=ADDR, ws_bytes=n.value)[0] == UNSUPPORTED
-    assert lib.fluid_w4_matmul_workspace(ref(w), 16, 0, C.byref(n)) == 0 and n.value == 0
+    assert lib.fluid_w4_matmul_workspace(ref(w), x(40), 1, C.byref(n)) == 0 and matmul(**kw, gate=ADDR, ws_bytes=n.value)[0] == UNSUPPORTED
+    for rows, dtype in ((16, F.BF16), (16, F.F32), (32, F.BF16)):
+        assert lib.fluid_w4_matmul_workspace(ref(w), x(rows, dtype), 0, C.byref(n)) == 0 and n.value == 0
+    assert lib.fluid_w4_matmul_workspace(ref(w), x(32, F.F32), 0, C.byref(n)) == 0 and n.value > 0
     kw = dict(w=w, xd=matrix(rows=16, cols=8192), od=matrix(rows=16, cols=512))
     assert matmul(**kw, ws=None, ws_bytes=0)[0] == UNSUPPORTED
-    for bad in ((w, 0, 0), (w, 40, 2), (shape(group=5), 40, 0)):
+    for bad in ((w, x(0), 0), (w, x(40), 2), (shape(group=5), x(40), 0), (w, None, 0), (w, x(40, 2), 0),
+                (w, ref(matrix(rows=40, cols=8191)), 0)):
         assert lib.fluid_w4_matmul_workspace(ref(bad[0]), bad[1], bad[2], C.byref(n)) == INVALID
-    assert lib.fluid_w4_matmul_workspace(ref(w), 40, 0, None) == INVALID
+    assert lib.fluid_w4_matmul_workspace(ref(w), x(40), 0, None) == INVALID
 
 
 def test_packing_and_reading_refusals():

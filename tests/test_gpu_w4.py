@@ -171,6 +171,17 @@ def test_strides_dimensions_and_outputs(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M", [1, 4, 5, 16, 20, 32, 33])
+def test_two_tiles_to_a_workgroup(dtype, M):
+    """So many rows of the matrix that workgroups have two tiles; the last has one."""
+    N, group = 16 * 513 - 3, 64
+    for K, pad in ((300, 0), (301, 0), (1500, 7)):
+        parts = matrix(K, N, K, group)
+        x = rand(3, M, K + pad, dtype=dtype)[:, :K]
+        check(W.w4_matmul(x, w4_of(*parts, group)), x, parts, group, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("M", [1, 3, 16, 21, 40])
 def test_rows_of_every_length_and_alignment(dtype, M):
     """Pieces of eight channels that end with the row, words that start between two
