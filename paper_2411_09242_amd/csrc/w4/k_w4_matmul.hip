@@ -9,7 +9,7 @@
 // the gated product with two of 11008 x 4096 (48 MB) 10.5 us (4.6 TB/s).  Every
 // workgroup reads x from L2, 256 bytes of a row at once: 16 rows times 4096 x 11008 take
 // 9.6 us (15.3 in the pieces of 64 bytes that operands are), 32 rows 14.4, where that
-// is half the time.  Small ones are the launch and two rounds of loads, 4.6 to 4.9 us.
+// is half the time.  Small ones are the launch and two rounds of loads, 4.5 to 5.1 us.
 #include "launch_w4.h"
 #include "w4_tile.h"
 
