@@ -216,11 +216,10 @@ fluid_status fluid_rotate(const fluid_rotary* r, const uint64_t* turns, const in
  * rows of out behind them are left as they are, and rows of q, k, v and g behind
  * them are not used.  out must not overlap an input.  workspace: as fluid_attention.
  * Arithmetic: fp32 sums and states.  fp32: fp32 products.  bf16: products on the
- * bf16 matrix cores; the state's own are exact to 2^-23, out's factors (q k with
- * its decay, and the state) are two bf16 parts each, 2^-16.  What is not finite in
- * q makes its row not finite, in k, v and state its channels of that and all later
- * rows and of the last state, where NaN may stand for an infinity, and a decay that
- * is NaN or infinite upwards all of them; rows before it stay.  Errors:
+ * bf16 matrix cores, whose factors are exact to 2^-23 (three bf16 parts).  What is
+ * not finite in q makes its row not finite, in k, v and state its channels of that
+ * and all later rows and of the last state, where NaN may stand for an infinity, and
+ * a decay that is NaN or infinite upwards all of them; rows before it stay.  Errors:
  * FLUID_E_INVALID; FLUID_E_ARENA_TOO_SMALL (workspace). */
 fluid_status fluid_linear_attention_workspace(const fluid_tokens* qd, const fluid_tokens* kd, uint64_t* bytes);
 fluid_status fluid_linear_attention(float scale, const fluid_tokens* qd, const void* q, const fluid_tokens* kd,

@@ -33,9 +33,10 @@
 // runs 141 and 150; without the loads of later chunks ahead 345.  512 heads of 1024
 // tokens, in one launch: 164 us (3.3 TB/s).
 //
-// bf16: S and the weighted products are two bf16 parts (cut off, and the rest
-// rounded: 2^-16), v with its decay three (2^-24): S is as exact as with fp32
-// products.  fp32: the fp32 matrix cores.
+// bf16: S, the weighted products and v with its decay are three bf16 parts each (the
+// first two cut off, the rest rounded: 2^-24), as exact as with fp32 products.  In
+// two parts (2^-16) the rows of 8192 tokens were four times as far from the rounded
+// exact ones, and took 121 us where they take 129.  fp32: the fp32 matrix cores.
 #include <type_traits>
 
 #include "dev_attn.h"
@@ -82,7 +83,7 @@ struct Core;
 template <int D>
 struct Core<uint16_t, D> {
   static constexpr int C = 64, KS = 32, LD = D + 16;  // tokens of a chunk; a row's elements in LDS, 8 banks apart: 16 % of its cycles are conflicts (12: 42 %)
-  static constexpr int PS = 2, PP = 2, PV = 3;       // parts of S, of the weighted products, of v
+  static constexpr int PS = 3, PP = 3, PV = 3;       // parts of S, of the weighted products, of v
   typedef u32x4 Frag;
   __device__ static __forceinline__ f32x4 mma(Frag a, Frag b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
