@@ -39,8 +39,9 @@ LinearParams plan_linear(const fluid_tokens* qd, const fluid_tokens* kd) {
   p.segments = (int32_t)((chunks + each - 1) / each);
   // every query head's workgroups read the states of the runs before theirs: 32 heads
   // over 8 key heads in 16 runs 104 us, with a scan between the launches 94; 64 heads
-  // in 8 runs 34 and 36
-  p.scan = int64_t(p.group) * p.segments > 24;
+  // in 8 runs 34 and 36.  One run has nothing before it; with more there are at most
+  // 256 states, rows of the scan's grid.
+  p.scan = p.segments > 1 && int64_t(p.group) * p.segments > 24;
   return p;
 }
 uint64_t workspace_of(const LinearParams& p, int head_dim) {

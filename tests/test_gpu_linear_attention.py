@@ -305,3 +305,56 @@ def test_on_another_stream():
     torch.cuda.current_stream().wait_stream(s)
     want = A.linear_attention(q, k, v, g)
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [3, 40])
+def test_many_heads_to_one_state_in_one_run(dtype, T):
+    """So few tokens that a run has them all, which leaves nothing to add up."""
+    B, H, D = 2, 28, 64
+    q, k, v = rand(1, B, T, H, D, dtype=dtype), rand(2, B, T, 1, D, dtype=dtype), rand(3, B, T, 1, D, dtype=dtype)
+    g, state, counts = decays(4, B, T, 1, True), rand(5, B, 1, D, D), [T, T - 2]
+    apart, out, mine = torch.full_like(q, 9.0), torch.full_like(q, 9.0), state.clone()
+    want = A.linear_attention(q, k, v, g, state=state, count=ints(counts), scale=0.1, out=apart)
+    check(want, q, k, v, g, state, counts, 0.1, dtype)
+    A.linear_attention(q, k, v, g, state=mine, state_out=mine, count=ints(counts), scale=0.1, out=out)
+    assert torch.equal(out, apart) and torch.equal(mine, want[1])
+
+
+def launches(call):
+    """Kernels that a call launches, by the nodes of a captured graph."""
+    import ctypes as C
+    graph = torch.cuda.CUDAGraph(keep_graph=True)
+    with torch.cuda.graph(graph):
+        call()
+    n = C.c_size_t()
+    assert fluid_hip().hipGraphGetNodes(C.c_void_p(graph.raw_cuda_graph()), None, C.byref(n)) == 0
+    return n.value
+
+
+def fluid_hip():
+    """The HIP runtime that the library's launches go to."""
+    import ctypes as C
+    return C.CDLL(F._L()._name)
+
+
+@pytest.mark.parametrize("H, T, want", [(28, 40, 2), (4, 40, 2), (12, 900, 3), (1, 900, 2), (1, 40, 1), (28, 1, 1)])
+def test_states_are_added_up_only_where_there_are_runs(H, T, want):
+    """One run in place: its first state is put apart, and the outputs follow. More
+    runs of many heads: a launch between the two that adds up."""
+    q, k = rand(1, 1, T, H, 64, dtype="bf16"), rand(2, 1, T, 1, 64, dtype="bf16")
+    g, state, out = decays(4, 1, T, 1, False), rand(5, 1, 1, 64, 64), torch.zeros_like(q)
+    ws = torch.empty(max(A.linear_attention_workspace(q, k), 1), dtype=torch.uint8, device="cuda")
+    call = lambda: A.linear_attention(q, k, k, g, state=state, state_out=state, out=out, workspace=ws)  # noqa: E731
+    call()
+    assert launches(call) == want
+
+
+def test_seventy_thousand_states_in_place():
+    B, T, Hk, group, D = 2200, 3, 32, 28, 32
+    q, k, v = rand(1, B, T, Hk, D, dtype="bf16"), rand(2, B, T, Hk, D, dtype="bf16"), rand(3, B, T, Hk, D, dtype="bf16")
+    q = torch.cat([q * (0.5 + i / group) for i in range(group)], 3).view(B, T, Hk * group, D)
+    g, state = decays(4, B, T, Hk, False), rand(5, B, Hk, D, D)
+    mine = state.clone()
+    got = A.linear_attention(q, k, v, g, state=mine, state_out=mine, scale=0.1)
+    check(got, q, k, v, g, state, [T] * B, 0.1, "bf16", heads=[(0, 0), (B - 1, Hk - 1), (1234, 7)])
