@@ -183,9 +183,10 @@ typedef struct {
 
 /* The turns that each pair makes from a position to the next, theta_i / (2 pi)
  * in units of 2^-64 modulo whole turns, into turns[dim / 2] in host memory; the
- * caller copies them to the device once.  Multiplied by any int32 position modulo
- * 2^64 they leave the angle within 2^-33 of a turn.  Needs no GPU.  Errors:
- * FLUID_E_INVALID. */
+ * caller copies them to the device once.  They are within one unit where theta_i is at
+ * most 1, as it is with factors of 1 and more: multiplied by any int32 position modulo
+ * 2^64 they leave the angle within 2^-33 of a turn.  Larger ones are within theta_i
+ * units.  Needs no GPU.  Errors: FLUID_E_INVALID. */
 fluid_status fluid_rotary_turns(const fluid_rotary* r, uint64_t* turns);
 
 /* q [batch, T, heads, head_dim] and k [batch, T, kv_heads, head_dim] turned into

@@ -325,3 +325,39 @@ def test_oracle_bytes_and_values():
     assert (words[1, 1, 1, 0] >> 4) & 15 == n[17, 130]
     y, size = O.product(rng.standard_normal((3, 150)), n, s, b, 32)
     assert (size >= np.abs(y)).all()
+
+
+# --------------------------------------- bounds that the headers state, and sizes
+def exact_frequencies(dim, base=10000.0, scaling="none", factor=1.0, length=0.0, low=1.0, high=32.0):
+    """theta_i / (2 pi) and theta_i, in 60 digits."""
+    from decimal import Decimal as D, getcontext
+    getcontext().prec = 60
+    tau = 2 * D("3.14159265358979323846264338327950288419716939937510582097494")
+    base, factor = D(base), D(factor)
+    if scaling == "base":
+        base = base * factor ** (D(dim) / D(dim - 2))
+    for i in range(dim // 2):
+        theta = base ** (D(-2 * i) / D(dim))
+        if scaling == "linear":
+            theta /= factor
+        if scaling == "ramp":
+            kept = min(D(1), max(D(0), (D(length) * theta / tau - D(low)) / (D(high) - D(low))))
+            theta = kept * theta + (1 - kept) * theta / factor
+        yield theta / tau, theta
+
+
+@pytest.mark.parametrize("kw", [
+    dict(), dict(base=500000.0), dict(base=1.0), dict(base=1e300), dict(scaling="linear", factor=4.0),
+    dict(scaling="base", factor=8.0), dict(scaling="base", base=500000.0, factor=2.5),
+    dict(scaling="ramp", factor=8.0, length=8192, low=1.0, high=4.0),
+    dict(scaling="ramp", factor=32.0, length=4096, low=1.0, high=32.0),
+    dict(scaling="linear", factor=0.1), dict(scaling="linear", factor=1e-3), dict(scaling="linear", factor=1e-6),
+    dict(scaling="base", factor=0.01), dict(scaling="ramp", factor=0.25, length=8192, low=1.0, high=4.0)])
+@pytest.mark.parametrize("dim", [4, 30, 64, 128, 1024])
+def test_turns_are_within_the_units_that_the_header_states(kw, dim):
+    opt = dict(kw, scaling=A.SCALINGS[kw.get("scaling", "none")])
+    turns = (C.c_uint64 * (dim // 2))()
+    assert A._lib().fluid_rotary_turns(ref(desc(dim, **opt)), turns) == 0
+    for t, (turn, theta) in zip(turns, exact_frequencies(dim, **kw)):
+        off = abs(int(t) - (turn % 1) * 2 ** 64)
+        assert min(off, 2 ** 64 - off) <= max(1, theta), (t, turn, float(off))
