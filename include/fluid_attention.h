@@ -218,9 +218,11 @@ fluid_status fluid_rotate(const fluid_rotary* r, const uint64_t* turns, const in
  * them are not used.  out must not overlap an input.  workspace: as fluid_attention.
  * Arithmetic: fp32 sums and states.  fp32: fp32 products.  bf16: products on the
  * bf16 matrix cores, whose factors are exact to 2^-23 (three bf16 parts).  What is
- * not finite in q makes its row not finite, in k, v and state its channels of that
- * and all later rows and of the last state, where NaN may stand for an infinity, and
- * a decay that is NaN or infinite upwards all of them; rows before it stay.  Errors:
+ * not finite stays with its head, and NaN may stand for an infinity: in q, in its
+ * row; in v, in its channel of that and all later rows and of the state's rows; in k,
+ * in all channels of that and all later rows and in its channel's row of the state; in
+ * a value of the state, in its column of all rows and in itself; a decay that is NaN
+ * or infinite upwards, in all that follows.  Rows before it stay.  Errors:
  * FLUID_E_INVALID; FLUID_E_ARENA_TOO_SMALL (workspace). */
 fluid_status fluid_linear_attention_workspace(const fluid_tokens* qd, const fluid_tokens* kd, uint64_t* bytes);
 fluid_status fluid_linear_attention(float scale, const fluid_tokens* qd, const void* q, const fluid_tokens* kd,

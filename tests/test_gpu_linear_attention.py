@@ -358,3 +358,37 @@ def test_seventy_thousand_states_in_place():
     mine = state.clone()
     got = A.linear_attention(q, k, v, g, state=mine, state_out=mine, scale=0.1)
     check(got, q, k, v, g, state, [T] * B, 0.1, "bf16", heads=[(0, 0), (B - 1, Hk - 1), (1234, 7)])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T, heads, at", [(2, 1, 1), (3, 2, 1), (150, 1, 70), (900, 2, 333), (900, 7, 333)])
+@pytest.mark.parametrize("value", [float("inf"), float("nan")])
+def test_how_far_a_key_and_a_state_that_are_no_numbers_reach(dtype, T, heads, at, value):
+    """A key's channel: all channels of its row and later ones, and that row of the
+    state. A value of the state: its column of all rows, and itself."""
+    B, Hk, D = 2, 2, 64
+    q = rand(1, B, T, heads * Hk, D, dtype=dtype)
+    k, v = rand(2, B, T, Hk, D, dtype=dtype), rand(3, B, T, Hk, D, dtype=dtype)
+    g, state = decays(4, B, T, Hk, True).clamp(min=-5.0), rand(5, B, Hk, D, D)
+    run = lambda: A.linear_attention(q, k, v, g, state=state, scale=0.2)  # noqa: E731
+    clean = run()
+    mine, rest = slice(heads, 2 * heads), [c for c in range(D) if c != 5]
+
+    def others(out, last):
+        assert torch.equal(out[1], clean[0][1]) and torch.equal(out[0, :, :heads], clean[0][0, :, :heads])
+        assert torch.equal(last[1], clean[1][1]) and torch.equal(last[0, 0], clean[1][0, 0])
+
+    old = k[0, at, 1, 5].clone()
+    k[0, at, 1, 5] = value
+    out, last = run()
+    k[0, at, 1, 5] = old
+    others(out, last)
+    assert torch.equal(out[0, :at], clean[0][0, :at]) and not out[0, at:, mine].isfinite().any()
+    assert not last[0, 1, 5].isfinite().any() and torch.equal(last[0, 1][rest], clean[1][0, 1][rest])
+
+    state[0, 1, 9, 5] = value
+    out, last = run()
+    others(out, last)
+    assert not out[0, :, mine, 5].isfinite().any() and torch.equal(out[0, :, mine][..., rest], clean[0][0, :, mine][..., rest])
+    bad = ~last[0, 1].isfinite()
+    assert bad[9, 5] and bad.sum() == 1 and torch.equal(last[0, 1][~bad], clean[1][0, 1][~bad])
