@@ -194,8 +194,9 @@ fluid_status fluid_rotary_turns(const fluid_rotary* r, uint64_t* turns);
  * from dim to 1024.  Row i of sequence b is at position positions[b *
  * position_stride + i], or start[b] + i (start NULL: i); not both; negative ones
  * too.  Rows from count[b] on (NULL: T; clamped to [0, T]) are left as they are.
- * inverse 1 turns back, which is the gradient as well.  An output may be its own
- * input, with the same strides; else they must not overlap.  turns: device
+ * inverse 1 turns by the negative angles, times the same amplitude: the transpose,
+ * which is the gradient, and the way back where amplitude is 1.  An output may be
+ * its own input, with the same strides; else they must not overlap.  turns: device
  * memory, 8-byte aligned, what fluid_rotary_turns gave for r.  fp32 arithmetic,
  * rounded once.  Errors: FLUID_E_INVALID. */
 fluid_status fluid_rotate(const fluid_rotary* r, const uint64_t* turns, const int32_t* start,

@@ -547,9 +547,9 @@ def rotary(turns, q, k=None, start=None, positions=None, count=None, inverse=Fal
 
     Row i of sequence b is at position start[b] + i (None: i), or at positions[b,
     i].  Rows from count[b] on (None: T) are left as they are.  inverse: turned
-    back.  q_out, k_out: where to write, which may be q and k themselves
-    (allocated as zeros by default).  Returns (q_out, k_out), or q_out without a
-    k."""
+    back, times the amplitude as well: the transpose, which is the gradient.  q_out,
+    k_out: where to write, which may be q and k themselves (allocated as zeros by
+    default).  Returns (q_out, k_out), or q_out without a k."""
     if q_out is None:
         q_out = _zeros(q, stream)
     if k is not None and k_out is None:

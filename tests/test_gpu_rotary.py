@@ -186,3 +186,14 @@ def test_on_another_stream():
     out = A.rotary(rot, q, stream=s)
     torch.cuda.current_stream().wait_stream(s)
     assert torch.equal(out, A.rotary(rot, q))
+
+
+@pytest.mark.parametrize("inter", [False, True])
+def test_the_inverse_has_the_amplitude_too(inter):
+    """Turned and turned by the transpose, a pair comes back times amplitude^2: each
+    turn is off by 8 u A (|x| + |y|), the second also turns the first one's error."""
+    rot, x, s = A.Rotary(64, interleaved=inter, amplitude=1.5), rand(1, 1, 9, 2, 64), ints([1000])
+    got = host(A.rotary(rot, A.rotary(rot, x, start=s), start=s, inverse=True))
+    size = np.abs(host(x)).reshape(1, 9, 2, *((32, 2) if inter else (2, 32))).sum(-1 if inter else -2, keepdims=True)
+    tol = np.broadcast_to(32 * U * 2.25 * size, (1, 9, 2, *((32, 2) if inter else (2, 32)))).reshape(got.shape)
+    assert (np.abs(got - 2.25 * host(x)) <= tol).all()
