@@ -5,9 +5,19 @@ Tolerances.  u = 2^-24.  Sums that cancel: with integers that fp32 and bf16 hold
 whole, and decays and a scale of 1, the exact result is 0.  What is left are fp32
 roundings of partial sums: of n terms of size t, n u / 2 of at most sqrt(n) t each
 where signs are random, which add up as random errors do: u n t / 2, so u times the
-sum of sizes.  Factors in two bf16 parts (16 bits) leave 10 to 21 u of it."""
+sum of sizes.  Factors in two bf16 parts (16 bits) leave 10 to 21 u of it.
+
+Long prompts with random values, whose memories of 512 tokens reach over several runs.
+What a chunk of 64 tokens (fp32: 32) keeps of a state is within 2 u, the same at each
+chunk, and what counts at the end has passed half of a memory's 8 (16) chunks: 16 u =
+2^-20, beside which the roundings of sums, some u in all, are small.  A state rounded to
+bf16 is off by 1.7e-3, values in two bf16 parts by 5e-6.  bf16 rows are rounded
+by at most 2^-8 of their binade's least value, 2^-8 / sqrt(3) in the mean square, and the
+values of a binade are 1.47 of it: 2^-9 of themselves with what the sizes' spread adds."""
 import numpy as np
 import pytest
+
+from oracle import decoder_layers as O
 
 torch = pytest.importorskip("torch")
 from paper_2411_09242_amd import attention as A  # noqa: E402
@@ -77,3 +87,25 @@ def test_tokens_that_cancel(dtype, D, group):
     assert np.linalg.norm(host(out)[:, at]) <= U * np.linalg.norm(size[:, at])
     most = np.einsum("bjhk,bjhd->bhkd", np.abs(host(k)), np.abs(host(v)))
     assert np.linalg.norm(host(last)) <= U * np.linalg.norm(most)
+
+
+@pytest.mark.parametrize("dtype, T, H, Hk, D", [
+    ("bf16", 2048, 4, 4, 128), ("bf16", 2048, 2, 2, 32), ("f32", 1111, 4, 2, 128), ("f32", 2000, 2, 2, 32),  # runs folded
+    ("bf16", 1500, 8, 2, 64), ("bf16", 2048, 8, 1, 128), ("f32", 2000, 8, 2, 64)])  # runs added up by a launch
+@pytest.mark.parametrize("per_token", [False, True])
+def test_long_memories_keep_their_precision(dtype, T, H, Hk, D, per_token):
+    q, k, v = rand(1, 1, T, H, D, dtype=dtype), rand(2, 1, T, Hk, D, dtype=dtype), rand(3, 1, T, Hk, D, dtype=dtype)
+    g = torch.full((Hk,), -1 / 512).cuda()
+    if per_token:
+        g = (g * (0.5 + torch.rand(1, T, Hk, generator=torch.Generator().manual_seed(4)).cuda())).contiguous()
+    state = rand(5, 1, Hk, D, D) * 16
+    out, last = A.linear_attention(q, k, v, g, state=state, scale=0.125)
+    decay = np.broadcast_to(host(g).reshape(-1, Hk), (T, Hk))
+    for h in range(Hk):
+        rows = slice(h * H // Hk, (h + 1) * H // Hk)
+        o, S, _, _ = O.linear_attention(host(q)[0, :, rows], host(k)[0, :, h], host(v)[0, :, h], decay[:, h],
+                                        host(state)[0, h], 0.125)
+        off = np.linalg.norm(host(last)[0, h] - S) / np.linalg.norm(S)
+        assert off <= 2.0 ** -20, ("state", h, off)
+        off = np.linalg.norm(host(out)[0, :, rows] - o) / np.linalg.norm(o)
+        assert off <= (2.0 ** -9 if dtype == "bf16" else 2.0 ** -20), ("out", h, off)
