@@ -241,3 +241,57 @@ def test_on_another_stream():
     torch.cuda.current_stream().wait_stream(s)
     w1 = W.w4_pack(m, 32)
     assert torch.equal(w.packed, w1.packed) and torch.equal(y, W.w4_matmul(x, w1)) and torch.equal(v, W.w4_read(w1))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M", [1, 2, 4, 5])
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_an_output_head_of_few_rows(dtype, M, group):
+    """1025 tiles: from 1024 on up to four rows too have two tiles to a workgroup."""
+    N = 16 * 1025 - 3
+    for K, pad in ((300, 0), (301, 0), (520, 7)):
+        parts = matrix(K, N, K, group)
+        x, add = rand(3, M, K + pad, dtype=dtype)[:, :K], rand(5, M, N, dtype=dtype)
+        add = add if K == 301 else None
+        check(W.w4_matmul(x, w4_of(*parts, group), add=add), x, parts, group, dtype, add=add)
+
+
+@pytest.mark.parametrize("M, group", [(6, 32), (20, 128)])
+def test_two_tiles_in_other_groups(M, group):
+    N = 16 * 513 - 3
+    for dtype in DT:
+        parts = matrix(7, N, 301, group)
+        x = rand(3, M, 301, dtype=dtype)
+        check(W.w4_matmul(x, w4_of(*parts, group)), x, parts, group, dtype)
+
+
+@pytest.mark.parametrize("dtype, M", [("bf16", 40), ("bf16", 70), ("f32", 17)])
+@pytest.mark.parametrize("gated", [False, True])
+def test_graphs_of_products_in_runs_replay(dtype, M, gated):
+    """Products in two launches with a workspace: one graph with its own, two that
+    share the caller's, eager calls between the replays."""
+    N, K = 96, 4096
+    w, g = w4_of(*matrix(1, N, K, 64), 64), w4_of(*matrix(3, N, K, 64), 64) if gated else None
+    x, add = rand(1, M, K, dtype=dtype), rand(2, M, N, dtype=dtype)
+    need = W.w4_matmul_workspace(x, w, gated)
+    assert need > 0
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    outs = [torch.zeros(M, N, dtype=DT[dtype], device="cuda") for _ in range(3)]
+    W.w4_matmul(x, w, gate=g, add=add, out=outs[0])
+    graphs = []
+    for i, out in enumerate(outs):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            W.w4_matmul(x, w, gate=g, add=add if i < 2 else None, out=out, workspace=ws if i else None)
+    for i in range(4):
+        x.copy_(rand(20 + i, M, K, dtype=dtype))
+        for out in outs:
+            out.fill_(7.0)
+        ws.fill_(255)
+        for graph in graphs:
+            graph.replay()
+        want, plain = W.w4_matmul(x, w, gate=g, add=add), W.w4_matmul(x, w, gate=g, workspace=ws)
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0], want) and torch.equal(outs[1], want) and torch.equal(outs[2], plain)
+    with pytest.raises(F.FluidError, match="workspace"):
+        W.w4_matmul(x, w, gate=g, workspace=ws[:need - 256])
