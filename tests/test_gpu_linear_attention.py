@@ -392,3 +392,40 @@ def test_how_far_a_key_and_a_state_that_are_no_numbers_reach(dtype, T, heads, at
     assert not out[0, :, mine, 5].isfinite().any() and torch.equal(out[0, :, mine][..., rest], clean[0][0, :, mine][..., rest])
     bad = ~last[0, 1].isfinite()
     assert bad[9, 5] and bad.sum() == 1 and torch.equal(last[0, 1][~bad], clean[1][0, 1][~bad])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [32, 64, 128])
+@pytest.mark.parametrize("T, H", [(100, 6), (700, 6), (700, 14)])
+def test_rows_off_16_byte_addresses(dtype, D, T, H):
+    """In one run and in several, folded and added up by a launch."""
+    B, Hk = 2, 2
+    q, k, v = (laid_out(rand(i, B, T, h, D, dtype=dtype), "odd") for i, h in ((1, H), (2, Hk), (3, Hk)))
+    out = laid_out(torch.full((B, T, H, D), 9.0, dtype=DT[dtype], device="cuda"), "odd")
+    g, state, counts = decays(4, B, T, Hk, True), rand(5, B, Hk, D, D), [T, T - 60]
+    got = A.linear_attention(q, k, v, g, state=state, count=ints(counts), scale=0.5, out=out)
+    check(got, q, k, v, g, state, counts, 0.5, dtype)
+    assert (out._base[..., D + 1:] == 7.0).all() and (out._base[..., 0] == 7.0).all()
+    want = A.linear_attention(q.contiguous(), k.contiguous(), v.contiguous(), g, state=state, count=ints(counts), scale=0.5,
+                              out=torch.full((B, T, H, D), 9.0, dtype=DT[dtype], device="cuda"))
+    assert torch.equal(out, want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("beyond", [False, True])
+def test_tokens_as_far_apart_as_offsets_of_32_bits_go(dtype, beyond):
+    """The largest distance of tokens whose chunk has 32-bit offsets, and the next
+    one that rows on 16-byte addresses can have."""
+    T, H, D = 70, 2, 64
+    width = 2 ** 23 - D - (0 if beyond else 8)
+    buf = torch.zeros(T, width, dtype=DT[dtype], device="cuda")
+    views = [buf[:, 1024 * i:1024 * i + h * D].view(1, T, h, D) for i, h in enumerate((H, 1, 1, H))]
+    q, k, v, out = views
+    assert q.stride(1) == width and all(t.data_ptr() % 16 == 0 for t in views)
+    for i, t in enumerate((q, k, v)):
+        t.copy_(rand(i, *t.shape, dtype=dtype))
+    out.fill_(9.0)
+    g = decays(4, 1, T, 1, True)
+    got = A.linear_attention(q, k, v, g, scale=0.3, out=out)
+    check(got, q, k, v, g, None, [T], 0.3, dtype)
+    assert (buf[:, 4096:] == 0).all()
