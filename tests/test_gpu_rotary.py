@@ -197,3 +197,21 @@ def test_the_inverse_has_the_amplitude_too(inter):
     size = np.abs(host(x)).reshape(1, 9, 2, *((32, 2) if inter else (2, 32))).sum(-1 if inter else -2, keepdims=True)
     tol = np.broadcast_to(32 * U * 2.25 * size, (1, 9, 2, *((32, 2) if inter else (2, 32)))).reshape(got.shape)
     assert (np.abs(got - 2.25 * host(x)) <= tol).all()
+
+
+@pytest.mark.parametrize("dtype, D, H, Hk, T", [("f32", 64, 12, 12, 800), ("bf16", 96, 7, 1, 2800), ("f32", 128, 5, 3, 1100),
+                                                ("bf16", 64, 9, 2, 2800)])
+@pytest.mark.parametrize("how", [None, "odd"])
+def test_threads_of_several_heads(dtype, D, H, Hk, T, how):
+    """131072 threads with four heads each, or with those that are left."""
+    inter = D == 128
+    el = 2 if dtype == "bf16" else 4
+    assert 4 * T * (D * el // 16 // (1 if inter else 2)) * ((H + Hk + 3) // 4) >= 131072
+    rot = A.Rotary(D, base=500000.0, interleaved=inter)
+    q, k = rand(1, 4, T, H, D, dtype=dtype), rand(2, 4, T, Hk, D, dtype=dtype)
+    if how:
+        q, k = laid_out(q, how), laid_out(k, how)
+    qo, ko = A.rotary(rot, q, k, count=ints([T, T - 1, 1, 0]))
+    pos, counts = [range(T)] * 4, [T, T - 1, 1, 0]
+    check(qo, q, pos, counts, (O.frequencies(D, 500000.0), inter, 1.0), dtype=dtype)
+    check(ko, k, pos, counts, (O.frequencies(D, 500000.0), inter, 1.0), dtype=dtype)
