@@ -361,3 +361,29 @@ def test_turns_are_within_the_units_that_the_header_states(kw, dim):
     for t, (turn, theta) in zip(turns, exact_frequencies(dim, **kw)):
         off = abs(int(t) - (turn % 1) * 2 ** 64)
         assert min(off, 2 ** 64 - off) <= max(1, theta), (t, turn, float(off))
+
+
+def linear_need(qd, kd):
+    n = C.c_uint64()
+    assert A._lib().fluid_linear_attention_workspace(ref(qd), ref(kd), C.byref(n)) == 0
+    return n.value
+
+
+@pytest.mark.parametrize("shape, heads, places", [
+    (dict(batch=1, tokens=8192, head_dim=128), (4, 4), None),          # runs
+    (dict(batch=1, tokens=1200, head_dim=128), (2, 2), None),
+    (dict(batch=1, tokens=1200, head_dim=64, dtype=F.F32), (8, 2), None),
+    (dict(batch=3, tokens=40, head_dim=64), (4, 2), 1),                # one run of shared heads: a state each
+    (dict(batch=3, tokens=40, head_dim=64), (2, 2), 0),                # nothing is read by others than write it
+    (dict(batch=3, tokens=2, head_dim=64), (4, 2), 0)])
+def test_linear_attention_workspace_is_there_and_enough(shape, heads, places):
+    qd, kd = (tokens(**shape, heads=h, stride=(1 << 30, 1 << 16, 128)) for h in heads)
+    n, state = linear_need(qd, kd), shape["batch"] * heads[1] * (shape["head_dim"] ** 2 + 1) * 4
+    assert n % state == 0 and (n // state >= 2 if places is None else n == places * state)
+    if n:
+        assert linear(qd=qd, kd=kd, ws_bytes=n)[0] == UNSUPPORTED
+        for bad in (dict(ws_bytes=n - 1), dict(ws=None)):
+            st, msg = linear(qd=qd, kd=kd, **bad)
+            assert st == TOO_SMALL and "workspace" in msg
+        st, msg = linear(qd=qd, kd=kd, ws=ADDR + 64)
+        assert st == INVALID and "aligned" in msg
