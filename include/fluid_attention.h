@@ -196,9 +196,9 @@ fluid_status fluid_rotary_turns(const fluid_rotary* r, uint64_t* turns);
  * too.  Rows from count[b] on (NULL: T; clamped to [0, T]) are left as they are.
  * inverse 1 turns by the negative angles, times the same amplitude: the transpose,
  * which is the gradient, and the way back where amplitude is 1.  An output may be
- * its own input, with the same strides; else they must not overlap.  turns: device
- * memory, 8-byte aligned, what fluid_rotary_turns gave for r.  fp32 arithmetic,
- * rounded once.  Errors: FLUID_E_INVALID. */
+ * its own input, with the same strides; else it must not overlap q, k or the other
+ * output.  turns: device memory, 8-byte aligned, what fluid_rotary_turns gave for r.
+ * fp32 arithmetic, rounded once.  Errors: FLUID_E_INVALID. */
 fluid_status fluid_rotate(const fluid_rotary* r, const uint64_t* turns, const int32_t* start,
                           const int32_t* positions, int64_t position_stride, const int32_t* count, int32_t inverse,
                           const fluid_tokens* qd, const void* q, const fluid_tokens* qod, void* qo,

@@ -102,6 +102,10 @@ fluid_status fluid_rotate(const fluid_rotary* r, const uint64_t* turns, const in
       set_pair(p, 1, kd, k, kod, ko, "k", "k_out");
       require(kd->dtype == qd->dtype && kd->batch == qd->batch && kd->tokens == qd->tokens && kd->head_dim == qd->head_dim,
               "q and k must have one dtype, batch, tokens and head_dim");
+      // threads read these while others write
+      require(qo != ko, "q_out and k_out must not be the same");
+      require(qo != k, "q_out must not be k");
+      require(ko != q, "k_out must not be q");
     }
     require(r->dim <= qd->head_dim, "rotary: dim is larger than head_dim");
     require(positions == nullptr || qd->batch == 1 || (position_stride >= 0 && position_stride <= (int64_t(1) << 40)),

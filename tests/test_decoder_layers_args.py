@@ -387,3 +387,17 @@ def test_linear_attention_workspace_is_there_and_enough(shape, heads, places):
             assert st == TOO_SMALL and "workspace" in msg
         st, msg = linear(qd=qd, kd=kd, ws=ADDR + 64)
         assert st == INVALID and "aligned" in msg
+
+
+@pytest.mark.parametrize("bad, word", [
+    (dict(ko=ADDR + 4096), "same"), (dict(q=ADDR, k=ADDR, qo=ADDR, ko=ADDR), "same"), (dict(qo=ADDR + 8192), "q_out must not be k"),
+    (dict(ko=ADDR), "k_out must not be q"), (dict(k=ADDR, qo=ADDR), "q_out must not be k")])
+def test_rotary_refuses_outputs_that_others_read_or_write(bad, word):
+    st, msg = rotate(kd=tokens(), **bad)
+    assert st == INVALID and word in msg, (st, msg)
+
+
+def test_rotary_of_one_tensor_twice_and_in_place():
+    for kw in (dict(k=ADDR), dict(qo=ADDR, ko=ADDR + 8192), dict(qo=ADDR), dict(ko=ADDR + 8192)):
+        st, msg = rotate(kd=tokens(), **kw)
+        assert st == UNSUPPORTED and "host-only" in msg, (kw, msg)
