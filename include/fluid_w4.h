@@ -29,7 +29,8 @@ extern "C" {
  *     s = f16((hi - lo) / 15)   b = f16(lo - 16 s)
  *     n = s > 0 ? clamp(rint((c - b) / s) - 16, 0, 15) : 0
  * in fp32, ties to even, as the cache of fluid_attention.h holds its values.  A
- * group that holds an infinity or a NaN is (0, NaN).
+ * group that holds an infinity or a NaN is (0, NaN).  Groups whose values are all
+ * below 2^-14 lose precision with the float16 pair.
  *
  * Memory, 16-byte aligned: for every 16 rows and, within them, every 128
  * channels (the last ones padded) 64 x 4 32-bit words; word j of place 16 g + r
@@ -60,10 +61,10 @@ fluid_status fluid_w4_read(const fluid_w4* w, const void* packed, const fluid_ma
 /* out = x W^T, or SiLU(x G^T) * (x W^T) with a gate G of W's geometry, plus add
  * if there is one: x [M, cols], add and out [M, rows] of one dtype.  gate, add
  * (with ad): NULL for none.  out may be add itself with the same stride, and must
- * not overlap x.  Made for few rows: every 64 of them read the matrix again.
- * workspace: 256-byte aligned device memory of at least the bytes that
- * fluid_w4_matmul_workspace returns for x (0: NULL will do), for this call
- * alone while it runs.
+ * not overlap x, nor add in any other way.  Made for few rows: every 64 of them read
+ * the matrix again.  workspace: 256-byte aligned device memory of at least the bytes
+ * that fluid_w4_matmul_workspace returns for x (0: NULL will do), for this call alone
+ * while it runs.
  * Arithmetic: x times 16 + n on the bf16 matrix cores (fp32: n - 8, and x in three
  * bf16 parts, exact to 2^-23), fp32 sums over a group, which s and b then enter in
  * fp32; one rounding at the end.  A row of x that is not finite, or whose sums
