@@ -22,21 +22,23 @@
 // the last one's workgroups fold those before their run, in order; where those
 // are many, a launch between them makes each run's first state.
 //
-// 8192 tokens of 32 heads of 128, bf16, in 16 runs: 128 us, of them 39 for the runs'
-// states.  Keys and values are read twice, 400 MB in all, 86 us at the rate of a
-// copy.  A chunk takes 14000 cycles of a workgroup with another one beside it, at
-// 1.9 GHz of 2.4: products of keys and queries 24 %, S^T q 15 %, the sum over j 8 %,
-// the state 18 %, LDS and its barriers 25 %.  Matrix cores are busy for 20 us and
-// vector instructions for 30 of 85; what is left is the latency of LDS reads, one
-// after another, since 128 registers leave no room for more of them at once.  256
-// registers and one workgroup to a compute unit: 140 us, in 8 runs 126; 24 and 32
-// runs 141 and 150; without the loads of later chunks ahead 345.  512 heads of 1024
-// tokens, in one launch: 164 us (3.3 TB/s).
+// 8192 tokens of 32 heads of 128, bf16, in 16 runs: 129 to 140 us by card, 39 of them
+// for the runs' states.  Keys and values are read twice, 400 MB in all, 86 us at the
+// rate of a copy.  A chunk takes 15200 cycles of a workgroup with another one beside it:
+// products of keys and queries 22 %, S^T q 20 %, the sum over j 11 %, the state 19 %, LDS
+// and its barriers 18 %, results and the next loads 10 %.  Of the outputs' 100 us matrix
+// cores are busy for 24 and vector instructions for 35; what is left is the latency of
+// LDS reads, one after another, since 128 registers leave no room for more of them at
+// once.  512 heads of 1024 tokens, in one launch: 180 us (3.0 TB/s).  Measured with two
+// parts of S and of the weighted products, at 128 us: 256 registers and one workgroup to
+// a compute unit 140 us, in 8 runs 126; 24 and 32 runs 141 and 150; without the loads of
+// later chunks ahead 345.
 //
 // bf16: S, the weighted products and v with its decay are three bf16 parts each (the
 // first two cut off, the rest rounded: 2^-24), as exact as with fp32 products.  In
 // two parts (2^-16) the rows of 8192 tokens were four times as far from the rounded
-// exact ones, and took 121 us where they take 129.  fp32: the fp32 matrix cores.
+// exact ones, and took 121 us where they take 129 (130 and 140 on another card).
+// fp32: the fp32 matrix cores.
 #include <type_traits>
 
 #include "dev_attn.h"
@@ -82,7 +84,7 @@ struct Core;
 
 template <int D>
 struct Core<uint16_t, D> {
-  static constexpr int C = 64, KS = 32, LD = D + 16;  // tokens of a chunk; a row's elements in LDS, 8 banks apart: 16 % of its cycles are conflicts (12: 42 %)
+  static constexpr int C = 64, KS = 32, LD = D + 16;  // tokens of a chunk; a row's elements in LDS, 8 banks apart: 23 % of its cycles are conflicts (12: 42 %)
   static constexpr int PS = 3, PP = 3, PV = 3;       // parts of S, of the weighted products, of v
   typedef u32x4 Frag;
   __device__ static __forceinline__ f32x4 mma(Frag a, Frag b, f32x4 c) {

@@ -22,14 +22,14 @@ LinearParams plan_linear(const fluid_tokens* qd, const fluid_tokens* kd) {
   // a workgroup of 256 threads to 32 columns of a state
   const int64_t heads = product({p.batch, p.kv_heads});
   require(product({heads, kd->head_dim / 32, 256}) <= kMostThreads, "q: too large for one launch");
-  // Token after token where they are few: 4 tokens of 256 heads of 128 11.1 us, in a
-  // chunk 11.8; 8 of them 16.3 and 12.1; 2 tokens of 1024 heads 29.6 and 37.1.  The
-  // chunk's workgroups take a query head each: 3 tokens of four heads to a state
-  // (128 states) 12.7 and 11.2.
+  // Token after token where they are few: 4 tokens of 256 heads of 128 11.3 us, in a
+  // chunk 13.0; 8 of them 15.9 and 13.0; 2 tokens of 1024 heads 30 and 43.  The chunk's
+  // workgroups take a query head each: 3 tokens of four heads to a state (128 states)
+  // 12.5 and 13.3, 4 of them 16.0 and 15.7.
   if (p.tokens <= 2 || int64_t(p.tokens) * p.group <= 4) return p;
   // Runs of two chunks or more, that make two workgroups to a compute unit: 8192
-  // tokens of 32 heads of 128 take 130 us with 512, 140 with 256, 150 with 1024; 8 x 512
-  // ragged fp32 tokens of 16 heads of 64 30, 39 and 28.
+  // tokens of 32 heads of 128 take 140 us with 512, 145 with 256, 156 with 1024; 8 x 512
+  // ragged fp32 tokens of 16 heads of 64 30, 39 and 29.
   const int chunk = linear_chunk(qd->dtype);
   const int64_t chunks = (int64_t(p.tokens) + chunk - 1) / chunk;
   const int64_t runs = std::max<int64_t>(1, std::min<int64_t>(512 / (heads * p.group), chunks / 2));
@@ -38,7 +38,7 @@ LinearParams plan_linear(const fluid_tokens* qd, const fluid_tokens* kd) {
   p.run = (int32_t)(each * chunk);
   p.segments = (int32_t)((chunks + each - 1) / each);
   // every query head's workgroups read the states of the runs before theirs: 32 heads
-  // over 8 key heads in 16 runs 104 us, with a scan between the launches 94; 64 heads
+  // over 8 key heads in 16 runs 108 us, with a scan between the launches 101; 64 heads
   // in 8 runs 34 and 36.  One run has nothing before it; with more there are at most
   // 256 states, rows of the scan's grid.
   p.scan = p.segments > 1 && int64_t(p.group) * p.segments > 24;
